@@ -466,6 +466,123 @@ sscn_status sscn_softmax_nll(const void* logits, int64_t n, int32_t classes, ssc
                              const int32_t* labels, float* loss, void* dlogits, hipStream_t stream);
 
 /*
+ * sscn_label_scores -- what a per-site classifier (Sec. 5: linear layer and
+ * softmax on each active site) says about its sites.  Per row x of `classes`
+ * logits, with log p = x - log sum exp x:
+ *   logprob[r]         log p of class labels[r]; 0 where the label is negative
+ *                      (a site without one), NaN where it is >= classes
+ *   entropy[r]         -sum_k p_k log p_k
+ *   stats[r]           (m, L): m = max x, L = log sum exp(x - m)
+ *   top_index[r][j]    the j-th best class, j < top_k: by decreasing logit,
+ *                      ties to the lowest class, NaN above everything
+ *   top_logprob[r][j]  its log p
+ *   logits   n x classes in dtype, row stride ldz >= classes, any alignment
+ *            of its elements' size
+ *   labels   device int32, n; NULL with logprob NULL: no labels
+ *   top_k    0 .. min(16, classes); 0: top_index and top_logprob are not used
+ * Numbers are computed and written in fp32.  A class of logit -inf is
+ * excluded (log p = -inf); a row of nothing else has entropy 0, stats
+ * (-inf, 0) and every log p = -inf.  A NaN or +inf makes its row's entropy,
+ * L and log probabilities NaN.  Outputs are contiguous and may not overlap
+ * the inputs.  The same call gives the same bits.
+ *   workspace  device, 16-byte aligned, at least the bytes that
+ *              sscn_label_scores_workspace gives for these n, classes and
+ *              top_k (0: may be NULL), the call's own until its work is done
+ * Allocates nothing: the call can be captured into a graph, whose replays
+ * use the given workspace.  Asynchronous on `stream`.
+ */
+sscn_status sscn_label_scores(const void* logits, int64_t ldz, int64_t n, int32_t classes, sscn_dtype dtype,
+                              const int32_t* labels, int32_t top_k, float* logprob, float* entropy, float* stats,
+                              int32_t* top_index, float* top_logprob, void* workspace, int64_t workspace_bytes,
+                              hipStream_t stream);
+sscn_status sscn_label_scores_workspace(int64_t n, int32_t classes, int32_t top_k, int64_t* bytes /* host */);
+
+/*
+ * sscn_label_scores_backward -- gradient at the logits of
+ *   sum_r dlogprob[r] logprob[r] + dentropy[r] entropy[r]
+ *         + sum_j dtop[r][j] top_logprob[r][j]
+ * (each of the three nullable) from what sscn_label_scores gave on the same
+ * logits: stats, and entropy (with dentropy) and top_index (with dtop;
+ * n x top_k, entries in [0, classes), a class listed twice receives both
+ * gradients).  Rows without a label take nothing from dlogprob; a row of
+ * -inf only gets zeros; a label >= classes (where dlogprob is given) makes
+ * its row NaN.
+ *   dlogits  n x classes in dtype, row stride ldd >= classes; overwritten,
+ *            may not overlap the inputs; elements between the rows are left
+ */
+sscn_status sscn_label_scores_backward(const void* logits, int64_t ldz, int64_t n, int32_t classes, sscn_dtype dtype,
+                                       const int32_t* labels, const float* stats, const float* entropy,
+                                       int32_t top_k, const int32_t* top_index, const float* dlogprob,
+                                       const float* dentropy, const float* dtop, void* dlogits, int64_t ldd,
+                                       hipStream_t stream);
+
+/*
+ * Activation checkpoints in 8 bits.  The backward pass of a pre-activated
+ * unit (batch normalisation + ReLU, then a convolution) reads the unit's
+ * input x and its activations a.  Both follow from xhat = (x - mean) *
+ * invstd, which these calls keep in 8 bits: one signed code a value and one
+ * exponent byte per 32 channels of a row.
+ *   codes      device int8, n x c contiguous
+ *   exponents  device uint8, n x ceil(c / 32) contiguous: byte b of channels
+ *              [32 i, 32 i + 32) says that code q stands for q * 2^(b - 127)
+ * The step 2^e of a block is the least power of two from 2^-126 up with
+ * max |xhat| <= 126 * 2^e, and a code is xhat (in fp32) / 2^e rounded to the
+ * nearest whole number, ties to even, moved by one where the ReLU would
+ * otherwise pass the restored value but not the original, or the other way
+ * round: with gamma xhat' + beta > 0 for the mask, a backward pass from the
+ * codes masks what the forward masked (where gamma * invstd does not
+ * underflow).  A block in which some xhat is infinite or NaN has byte 255 and
+ * stands for NaN in all its channels.
+ * None of these calls allocates: they can be captured into a graph.
+ */
+
+/*
+ * sscn_batchnorm_relu_apply_q8 -- sscn_batchnorm_relu_apply (the same y, bit
+ * for bit; y may be x) that also writes codes and exponents.  mean, invstd
+ * and scale are those of sscn_batchnorm_forward.
+ */
+sscn_status sscn_batchnorm_relu_apply_q8(const void* x, int64_t ldx, int64_t n, int32_t c, sscn_dtype dtype,
+                                         const float* mean, const float* invstd, const float* scale,
+                                         const float* gamma, const float* beta, void* y, int64_t ldy, int8_t* codes,
+                                         uint8_t* exponents, hipStream_t stream);
+
+/* sscn_q8_values -- y = the values that the codes stand for (exact in bf16 too). */
+sscn_status sscn_q8_values(const int8_t* codes, const uint8_t* exponents, int64_t n, int32_t c, sscn_dtype dtype,
+                           void* y, int64_t ldy, hipStream_t stream);
+
+/*
+ * sscn_batchnorm_relu_backward_params_q8 -- sscn_batchnorm_relu_backward_params
+ * from the codes: with xhat' the value kept and dz = dA where gamma xhat' +
+ * beta > 0, else 0: dbeta = sum of dz, dgamma = sum of dz * xhat'.  If `a` is
+ * not NULL it receives the restored activations relu(gamma xhat' + beta) (NaN
+ * for a block that stands for NaN), which the convolution's weight gradient
+ * reads.  a may not overlap dA.
+ *   workspace  device, 8-byte aligned, at least the bytes that
+ *              ..._params_q8_workspace gives for n and c, the call's own until
+ *              its work is done
+ */
+sscn_status sscn_batchnorm_relu_backward_params_q8(const void* dA, int64_t ldd, const int8_t* codes,
+                                                   const uint8_t* exponents, int64_t n, int32_t c, sscn_dtype dtype,
+                                                   const float* gamma, const float* beta, float* dgamma, float* dbeta,
+                                                   void* a, int64_t lda, void* workspace, int64_t workspace_bytes,
+                                                   hipStream_t stream);
+sscn_status sscn_batchnorm_relu_backward_params_q8_workspace(int64_t n, int32_t c, int64_t* bytes /* host */);
+
+/*
+ * sscn_batchnorm_relu_backward_input_q8 -- the gradient at x from the codes,
+ *   dx = gamma * invstd * (dz - dbeta / n - xhat' * dgamma / n)  (+ add),
+ * for the channels [col0, col0 + cols) of the layer.  dA, the codes, the
+ * exponents and the vectors are the whole layer's (c channels); add
+ * (nullable) and dx hold the range's columns alone.  dx may be add.
+ */
+sscn_status sscn_batchnorm_relu_backward_input_q8(const void* dA, int64_t ldd, const int8_t* codes,
+                                                  const uint8_t* exponents, int64_t n, int32_t c, int32_t col0,
+                                                  int32_t cols, sscn_dtype dtype, const float* gamma,
+                                                  const float* beta, const float* invstd, const float* dgamma,
+                                                  const float* dbeta, const void* add, int64_t ld_add, void* dx,
+                                                  int64_t ldx_out, hipStream_t stream);
+
+/*
  * sscn_sgd_nesterov -- one step of SGD with Nesterov momentum and L2 weight
  * decay (Sec. 6.2), elementwise over `count` fp32 parameters:
  *   g' = g + weight_decay * p;  buf = momentum * buf + g';

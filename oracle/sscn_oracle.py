@@ -534,6 +534,122 @@ def softmax_nll(logits, labels):
     return loss, d / n
 
 
+def label_scores(logits, labels, top_k=0):
+    """Per site: log softmax(logits)[label] (0 for a negative label, NaN for
+    one >= classes), the entropy of the softmax, (max, log sum exp(x - max)),
+    and the top_k best classes (NaN first, then by decreasing logit, ties to
+    the lowest class) with their log probabilities.  Rows of -inf only:
+    entropy 0 and log sum 0; rows with NaN or +inf: NaN."""
+    z = np.asarray(logits, np.float64)
+    n, k = z.shape
+    with np.errstate(all="ignore"):
+        m = z.max(axis=1) if n else np.zeros(0)
+        empty = np.isneginf(m)
+        d = z - np.where(empty, 0.0, m)[:, None]
+        e = np.exp(d)
+        one = np.argmax(d, axis=1)[:, None] if n else np.zeros((0, 1), np.int64)
+        rest = e.copy()
+        np.put_along_axis(rest, one, 0.0, axis=1)
+        L = np.where(empty, 0.0, np.log1p(rest.sum(axis=1)))
+        L = np.where(np.isposinf(m) | np.isnan(m), np.nan, L)
+        logp = d - L[:, None]
+        H = np.where(empty, 0.0, L - np.where(e > 0, e * np.where(e > 0, d, 0.0), 0.0).sum(axis=1) / e.sum(axis=1))
+        H = np.where(np.isnan(L), np.nan, H)
+    order = np.argsort(np.where(np.isnan(z), -np.inf, -z), axis=1, kind="stable")
+    # NaN before +inf: both sort as -inf above, so NaN columns are moved to the front
+    first = np.argsort(~np.isnan(np.take_along_axis(z, order, axis=1)), axis=1, kind="stable")
+    top = np.take_along_axis(order, first, axis=1)[:, :top_k]
+    lp = None
+    if labels is not None:
+        labels = np.asarray(labels, np.int64)
+        got = logp[np.arange(n), np.clip(labels, 0, k - 1)]
+        lp = np.where(labels < 0, 0.0, np.where(labels >= k, np.nan, got))
+    return lp, H, np.stack([m, L], axis=1), top, np.take_along_axis(logp, top, axis=1)
+
+
+def label_scores_backward(logits, labels, dlogprob=None, dentropy=None, top=None, dtop=None):
+    """Gradient of label_scores' numbers (weighted by dlogprob, dentropy and
+    dtop, the last for the classes `top`) at the logits."""
+    z = np.asarray(logits, np.float64)
+    n, k = z.shape
+    _, H, stats, _, _ = label_scores(z, None)
+    empty = np.isneginf(stats[:, 0]) & (stats[:, 1] == 0)
+    logp = z - np.where(empty, 0.0, stats[:, 0])[:, None] - stats[:, 1:]
+    p = np.exp(logp)
+    A = np.zeros((n, k))
+    if dlogprob is not None:
+        labels = np.asarray(labels, np.int64)
+        g = np.where(labels < 0, 0.0, np.where(labels >= k, np.nan, dlogprob))
+        A[np.arange(n), np.clip(labels, 0, k - 1)] += g
+    if dtop is not None:
+        np.add.at(A, (np.arange(n)[:, None], top), dtop)
+    # d log p_j / dx_k = [j = k] - p_k;  dH / dx_k = -p_k (log p_k + H)
+    out = A - p * A.sum(axis=1, keepdims=True)
+    if dentropy is not None:
+        out -= np.asarray(dentropy, np.float64)[:, None] * p * np.where(p > 0, np.where(p > 0, logp, 0.0) + H[:, None], 0.0)
+    return np.where(empty[:, None], 0.0, out)
+
+
+# --------------------------------------------------------------------------
+# activation checkpoints in 8 bits
+# --------------------------------------------------------------------------
+Q8_BLOCK = 32
+
+
+def _q8_per_channel(per_block, c):
+    return np.repeat(per_block, Q8_BLOCK, axis=1)[:, :c]
+
+
+def q8_encode(x, mean, invstd, scale, gamma, beta):
+    """Codes (int8) and exponent bytes (uint8) of the normalised input of a
+    batch-normalised unit: xhat = (x - mean) * invstd in fp32; per row and 32
+    channels the least e >= -126 with max |xhat| <= 126 * 2^e; xhat / 2^e
+    rounded to nearest even, moved by one where gamma code 2^e + beta > 0
+    would differ from (x - mean) scale + beta > 0.  Byte e + 127; 255 with
+    codes 0 for a block with a value that is not finite."""
+    f = np.float32
+    n, c = x.shape
+    d = np.asarray(x, f) - np.asarray(mean, f)
+    with np.errstate(all="ignore"):
+        v = (d * np.asarray(invstd, f)).astype(np.float64)
+    codes, exps = np.zeros((n, c), np.int64), np.zeros((n, -(-c // Q8_BLOCK)), np.int64)
+    g, b, s = (np.asarray(t, np.float64) for t in (gamma, beta, scale))
+    for i in range(exps.shape[1]):
+        at = slice(Q8_BLOCK * i, min(c, Q8_BLOCK * (i + 1)))
+        good = np.isfinite(v[:, at]).all(axis=1)
+        most = np.where(good, np.abs(np.where(np.isfinite(v[:, at]), v[:, at], 0.0)).max(axis=1), 0.0)
+        e = np.full(n, -126)
+        while (most > 126 * np.ldexp(1.0, e)).any():
+            e += most > 126 * np.ldexp(1.0, e)
+        step = np.ldexp(1.0, e)[:, None]
+        q = np.rint(np.where(good[:, None], v[:, at], 0.0) / step)
+        with np.errstate(all="ignore"):
+            want = d[:, at].astype(np.float64) * s[at] + b[at] > 0
+        have = q * step * g[at] + b[at] > 0
+        q += (want.astype(int) - have.astype(int)) * np.sign(g[at])
+        codes[:, at] = np.where(good[:, None], q, 0)
+        exps[:, i] = np.where(good, e + 127, 255)
+    return codes.astype(np.int8), exps.astype(np.uint8)
+
+
+def q8_values(codes, exponents):
+    """What the codes stand for (NaN for the exponent byte 255)."""
+    per = np.where(exponents == 255, np.nan, np.ldexp(1.0, np.asarray(exponents, np.int64) - 127))
+    return np.asarray(codes, np.float64) * _q8_per_channel(per, codes.shape[1])
+
+
+def batch_norm_relu_backward_q8(dA, codes, exponents, gamma, beta, invstd):
+    """(a, dX, dgamma, dbeta) of relu(gamma xhat + beta) from the kept xhat."""
+    v = q8_values(codes, exponents)
+    g, b = np.asarray(gamma, np.float64), np.asarray(beta, np.float64)
+    n = v.shape[0]
+    pre = g * v + b
+    dz = np.where(pre > 0, np.asarray(dA, np.float64), 0.0)
+    dbeta, dgamma = dz.sum(axis=0), (dz * v).sum(axis=0)
+    dX = g * np.asarray(invstd, np.float64) * (dz - dbeta / max(n, 1) - v * dgamma / max(n, 1))
+    return np.where(pre <= 0, 0.0, pre), dX, dgamma, dbeta
+
+
 def sgd_nesterov(p, g, buf, lr, momentum=0.9, weight_decay=1e-4):
     """One SGD step with Nesterov momentum and L2 weight decay (Sec. 6.2):
     g' = g + wd p; buf' = momentum buf + g'; p' = p - lr (g' + momentum buf').

@@ -12,6 +12,7 @@ import ctypes
 import os
 import re
 import threading
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -84,6 +85,18 @@ _SIGS = {
     "sscn_column_sum": [_vp, _i64, _i64, _i32, ctypes.c_int, _vp, _vp],
     "sscn_add": [_vp, _i64, _vp, _i64, _i64, _i32, ctypes.c_int, _vp, _i64, _vp],
     "sscn_softmax_nll": [_vp, _i64, _i32, ctypes.c_int, _vp, _vp, _vp, _vp],
+    "sscn_label_scores": [_vp, _i64, _i64, _i32, ctypes.c_int, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp],
+    "sscn_label_scores_workspace": [_i64, _i32, _i32, _vp],
+    "sscn_label_scores_backward": [_vp, _i64, _i64, _i32, ctypes.c_int, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp,
+                                   _i64, _vp],
+    "sscn_batchnorm_relu_apply_q8": [_vp, _i64, _i64, _i32, ctypes.c_int, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp,
+                                     _vp, _vp],
+    "sscn_q8_values": [_vp, _vp, _i64, _i32, ctypes.c_int, _vp, _i64, _vp],
+    "sscn_batchnorm_relu_backward_params_q8": [_vp, _i64, _vp, _vp, _i64, _i32, ctypes.c_int, _vp, _vp, _vp, _vp, _vp,
+                                               _i64, _vp, _i64, _vp],
+    "sscn_batchnorm_relu_backward_params_q8_workspace": [_i64, _i32, _vp],
+    "sscn_batchnorm_relu_backward_input_q8": [_vp, _i64, _vp, _vp, _i64, _i32, _i32, _i32, ctypes.c_int, _vp, _vp,
+                                              _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp],
     "sscn_sgd_nesterov": [_vp, _vp, _vp, _i64, ctypes.c_float, ctypes.c_float, ctypes.c_float, _vp, _vp],
     "sscn_sgd_nesterov_many": [_vp, _i32, ctypes.c_float, ctypes.c_float, ctypes.c_float, _vp],
     "sscn_time_next_launch": [_vp, _vp],
@@ -608,6 +621,186 @@ def softmax_nll(logits, labels):
         _check(lib().sscn_softmax_nll(_vp_of(logits), n, k, _dtype_code(logits), _vp_of(labels), _vp_of(loss),
                                       _vp_of(d), _stream(logits)))
     return loss, d
+
+
+class LabelScores(NamedTuple):
+    """label_scores' results, per row: log probability of the label (None
+    without labels), entropy, statistics (maximum, log sum exp of the logits
+    less the maximum), the best classes and their log probabilities (None for
+    top_k = 0)."""
+    logprob: Optional[torch.Tensor]
+    entropy: torch.Tensor
+    stats: torch.Tensor
+    top_index: Optional[torch.Tensor]
+    top_logprob: Optional[torch.Tensor]
+
+
+def _rows(t, name, dtype=None, device=None):
+    """_mat for rows that do not overlap, on one device."""
+    p, ld = _mat(t, name, dtype)
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} must be on {device}")
+    if t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"{name}: rows overlap")
+    return p, ld
+
+
+def _on(t, name, dtype, shape, device):
+    """Pointer of a contiguous tensor of this type, shape and device."""
+    t = _dev_tensor(t, name, dtype)
+    if tuple(t.shape) != tuple(shape) or t.device != device:
+        raise ValueError(f"{name} must be a {tuple(shape)} tensor on {device}")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _workspace(query, *sizes, device):
+    """A workspace of the size that `query` gives, from torch's allocator (so
+    a captured graph owns the ones of its calls)."""
+    need = ctypes.c_int64()
+    _check(query(*sizes, ctypes.byref(need)))
+    return torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
+
+
+def label_scores(logits, labels=None, top_k=0):
+    """Scores of per-site logits (n x classes, rows may be strided) -> LabelScores.
+
+    labels: int32 (n,), negative for a site without a label (log probability
+    0), or None; a label >= classes gives NaN.  top_k: best classes to list,
+    at most min(16, classes), ties to the lowest class."""
+    zp, ldz = _rows(logits, "logits")
+    n, k = logits.shape
+    dev, top_k = logits.device, int(top_k)
+    lp = _on(labels, "labels", torch.int32, (n,), dev) if labels is not None else None
+    new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=dev)
+    L = lib()
+    work = _workspace(L.sscn_label_scores_workspace, n, k, top_k, device=dev)
+    out = LabelScores(new(n) if labels is not None else None, new(n), new(n, 2),
+                      new(n, top_k, dtype=torch.int32) if top_k else None, new(n, top_k) if top_k else None)
+    with torch.cuda.device(dev):
+        _check(L.sscn_label_scores(zp, ldz, n, k, _dtype_code(logits), lp, top_k, *[_vp_of(t) for t in out],
+                                   _vp_of(work), work.numel() if work is not None else 0, _stream(logits)))
+    return out
+
+
+def label_scores_backward(logits, scores, labels=None, dlogprob=None, dentropy=None, dtop=None, out=None):
+    """dlogits of label_scores' numbers, given the gradients at its logprob
+    (n,), entropy (n,) and top_logprob (n, top_k), each fp32 or None."""
+    zp, ldz = _rows(logits, "logits")
+    n, k = logits.shape
+    dev, f32 = logits.device, torch.float32
+    top_k = scores.top_index.shape[1] if dtop is not None and scores.top_index is not None else 0
+    if dtop is not None and top_k == 0:
+        raise ValueError("dtop without the best classes")
+    if dlogprob is not None and labels is None:
+        raise ValueError("dlogprob without labels")
+    if out is None:
+        out = torch.empty((n, k), dtype=logits.dtype, device=dev)
+    op, ldo = _rows(out, "out", logits.dtype, dev)
+    if tuple(out.shape) != (n, k):
+        raise ValueError("out must match logits")
+    opt = lambda t, name, dtype, *shape: _on(t, name, dtype, shape, dev) if t is not None else None
+    args = [opt(labels, "labels", torch.int32, n), _on(scores.stats, "stats", f32, (n, 2), dev),
+            _on(scores.entropy, "entropy", f32, (n,), dev), top_k,
+            _on(scores.top_index, "top_index", torch.int32, (n, top_k), dev) if top_k else None,
+            opt(dlogprob, "dlogprob", f32, n), opt(dentropy, "dentropy", f32, n), opt(dtop, "dtop", f32, n, top_k)]
+    with torch.cuda.device(dev):
+        _check(lib().sscn_label_scores_backward(zp, ldz, n, k, _dtype_code(logits), *args, op, ldo, _stream(logits)))
+    return out
+
+
+Q8_BLOCK = 32  # channels that share an exponent byte
+
+
+class Q8(NamedTuple):
+    """A normalised input kept in 8 bits: codes (n, c) int8, exponents
+    (n, ceil(c / 32)) uint8; code q of exponent b stands for q * 2^(b - 127)."""
+    codes: torch.Tensor
+    exponents: torch.Tensor
+
+
+def _q8(q8):
+    codes = _dev_tensor(q8.codes, "codes", torch.int8)
+    if codes.dim() != 2:
+        raise ValueError("codes must be n x c")
+    n, c = codes.shape
+    return (ctypes.c_void_p(codes.data_ptr()),
+            _on(q8.exponents, "exponents", torch.uint8, (n, -(-c // Q8_BLOCK)), codes.device))
+
+
+def batchnorm_relu_apply_q8(x, st, gamma, beta, out=None):
+    """batchnorm_relu_apply(x, st, beta) that also keeps the normalised input
+    in 8 bits -> (activations, Q8)."""
+    xp, ldx = _rows(x, "x")
+    n, c = x.shape
+    dev = x.device
+    if out is None:
+        out = torch.empty((n, c), dtype=x.dtype, device=dev)
+    op, ldo = _rows(out, "out", x.dtype, dev)
+    if tuple(out.shape) != (n, c):
+        raise ValueError("out must match x")
+    q8 = Q8(torch.empty((n, c), dtype=torch.int8, device=dev),
+            torch.empty((n, -(-c // Q8_BLOCK)), dtype=torch.uint8, device=dev))
+    v = lambda t, name: _on(t, name, torch.float32, (c,), dev)
+    with torch.cuda.device(dev):
+        _check(lib().sscn_batchnorm_relu_apply_q8(xp, ldx, n, c, _dtype_code(x), v(st.mean, "mean"),
+                                                  v(st.invstd, "invstd"), v(st.scale, "scale"), v(gamma, "gamma"),
+                                                  v(beta, "beta"), op, ldo, _vp_of(q8.codes), _vp_of(q8.exponents),
+                                                  _stream(x)))
+    return out, q8
+
+
+def q8_values(q8, dtype=torch.float32):
+    """The normalised input that a Q8 stands for, float32 or bfloat16 (exact
+    in both)."""
+    qp = _q8(q8)
+    n, c = q8.codes.shape
+    out = torch.empty((n, c), dtype=dtype, device=q8.codes.device)
+    with torch.cuda.device(out.device):
+        _check(lib().sscn_q8_values(*qp, n, c, _dtype_code(out), _vp_of(out), c, _stream(out)))
+    return out
+
+
+def batchnorm_relu_backward_params_q8(dA, q8, gamma, beta, restore=False):
+    """(dgamma, dbeta, a) of batchnorm_relu_apply_q8 given dA; a: the
+    activations restored from the codes (restore=True; else None)."""
+    qp = _q8(q8)
+    n, c = q8.codes.shape
+    dev = q8.codes.device
+    dp, ldd = _rows(dA, "dA", None, dev)
+    if tuple(dA.shape) != (n, c):
+        raise ValueError("dA must match the codes")
+    v = lambda t, name: _on(t, name, torch.float32, (c,), dev)
+    dg, db = (torch.empty(c, dtype=torch.float32, device=dev) for _ in range(2))
+    a = torch.empty((n, c), dtype=dA.dtype, device=dev) if restore else None
+    L = lib()
+    work = _workspace(L.sscn_batchnorm_relu_backward_params_q8_workspace, n, c, device=dev)
+    with torch.cuda.device(dev):
+        _check(L.sscn_batchnorm_relu_backward_params_q8(dp, ldd, *qp, n, c, _dtype_code(dA), v(gamma, "gamma"),
+                                                        v(beta, "beta"), _vp_of(dg), _vp_of(db), _vp_of(a), c,
+                                                        _vp_of(work), work.numel(), _stream(dA)))
+    return dg, db, a
+
+
+def batchnorm_relu_backward_input_q8(dA, q8, gamma, beta, invstd, dgamma, dbeta, out, add=None, cols=None):
+    """out = gradient at the unit's input (columns `cols` = (lo, hi) of the
+    layer, default all) plus `add`; out / add hold just those columns."""
+    qp = _q8(q8)
+    n, c = q8.codes.shape
+    dev = q8.codes.device
+    lo, hi = cols if cols is not None else (0, c)
+    dp, ldd = _rows(dA, "dA", None, dev)
+    op, ldo = _rows(out, "out", dA.dtype, dev)
+    ap, lda = _rows(add, "add", dA.dtype, dev) if add is not None else (None, 0)
+    if tuple(dA.shape) != (n, c):
+        raise ValueError("dA must match the codes")
+    if tuple(out.shape) != (n, hi - lo) or (add is not None and tuple(add.shape) != (n, hi - lo)):
+        raise ValueError("out and add must hold the selected columns")
+    v = lambda t, name: _on(t, name, torch.float32, (c,), dev)
+    with torch.cuda.device(dev):
+        _check(lib().sscn_batchnorm_relu_backward_input_q8(
+            dp, ldd, *qp, n, c, lo, hi - lo, _dtype_code(dA), v(gamma, "gamma"), v(beta, "beta"), v(invstd, "invstd"),
+            v(dgamma, "dgamma"), v(dbeta, "dbeta"), ap, lda, op, ldo, _stream(dA)))
+    return out
 
 
 def _check_sgd(params, grads, buf, params_bf16):

@@ -11,8 +11,11 @@ parameter by SGD with Nesterov momentum and L2 weight decay (Sec. 6.2:
 momentum 0.9, weight decay 1e-4, learning rate 0.1).
 
 Every arithmetic step runs in libsscn.so; this module orders the calls and
-keeps the tensors the backward pass needs (each unit's input and its
-pre-activated input, and the batch statistics).  Parameters are kept in
+keeps the tensors the backward pass needs: the batch statistics, and each
+unit's input and its pre-activated input (keep="full") or, in their place,
+its normalised input in 8 bits, from which the backward pass restores both
+(keep="q8": a quarter of the bytes of a bf16 network's tape, an eighth of an
+fp32 one's).  Parameters are kept in
 fp32 (the master copy the update works on); a bf16 network convolves with a
 bf16 copy of its weights, which the update refreshes.
 """
@@ -55,30 +58,63 @@ class Params:
         return list(self.master)
 
 
-def _bn_relu(name, x, P, tape_entry):
+def _bn_relu(name, x, P, tape_entry, keep):
     gamma, beta = P.master[name][0], P.master[name][1]
     rm, rv = P.running[name]
     st = sscn.batchnorm_forward(x, gamma, beta, running_mean=rm, running_var=rv)
-    a = sscn.batchnorm_relu_apply(x, st, beta)
-    tape_entry.update(x=x, a=a, st=st)
+    if keep == "q8":
+        a, q8 = sscn.batchnorm_relu_apply_q8(x, st, gamma, beta)
+        tape_entry.update(q8=q8, st=st)
+    else:
+        a = sscn.batchnorm_relu_apply(x, st, beta)
+        tape_entry.update(x=x, a=a, st=st)
     return a
 
 
-def _bn_relu_back(name, da, e, P, outs):
-    """outs: [(tensor, (lo, hi), add or None)] column ranges of the gradient at e["x"]."""
+def _unit_back(name, dy, e, rb, P, outs):
+    """Backward pass of one unit (or of the head).  outs: [(tensor, (lo, hi) or
+    None, add or None)], column ranges of the gradient at the unit's input.
+    Returns (da, [dgamma, dbeta, dW]); from a kept q8, e["a"] becomes the
+    restored activations."""
     gamma, beta = P.master[name][0], P.master[name][1]
-    dg, db = sscn.batchnorm_relu_backward_params(da, e["x"], e["st"], beta)
-    for out, cols, add in outs:
-        sscn.batchnorm_relu_backward_input(da, e["x"], gamma, beta, e["st"], dg, db, out, add=add, cols=cols)
-    return dg, db
+    W, st = P.compute[name], e["st"]
+    if "q8" in e:
+        # the restored activations come out of the pass that the parameter
+        # gradients make over dA and the codes, so dA first, then dW
+        da, _ = sscn.sparse_conv_backward(None, W, dy, rb, wgrad=False)
+        dg, db, e["a"] = sscn.batchnorm_relu_backward_params_q8(da, e["q8"], gamma, beta, restore=True)
+        _, dW = sscn.sparse_conv_backward(e["a"], W, dy, rb, dgrad=False)
+        for out, cols, add in outs:
+            sscn.batchnorm_relu_backward_input_q8(da, e["q8"], gamma, beta, st.invstd, dg, db, out, add=add, cols=cols)
+    else:
+        da, dW = sscn.sparse_conv_backward(e["a"], W, dy, rb)
+        dg, db = sscn.batchnorm_relu_backward_params(da, e["x"], st, beta)
+        for out, cols, add in outs:
+            sscn.batchnorm_relu_backward_input(da, e["x"], gamma, beta, st, dg, db, out, add=add, cols=cols)
+    return da, [dg, db, dW]
 
 
-def train_step(x, labels, geom, P, lr=0.1, momentum=0.9, weight_decay=1e-4, update=True, trace=None):
+def train_step(x, labels, geom, P, lr=0.1, momentum=0.9, weight_decay=1e-4, update=True, trace=None, keep="full",
+               objective=None, top_k=0):
     """Forward, backward and (if `update`) the SGD step on level-0 features
     x (n_0 x C_0, the network's dtype) and int32 labels (n_0).  Returns
     (loss (device fp32 scalar), grads {name: [dgamma, dbeta, dW(, dbias)]},
     fp32).  If `trace` is a dict it receives, per unit name, the tensors of
-    that unit: x, a (its pre-activated input), y (its output), dy, da, dx."""
+    that unit: x, a (its pre-activated input), y (its output), dy, da, dx.
+
+    keep: what the backward pass finds of each unit's forward, "full" (x and
+    a) or "q8" (the normalised input in 8 bits; `trace` then has q8 in place
+    of x, and a is the restored one).
+
+    objective: None for the mean negative log-likelihood, every site
+    labelled; else a callable that is given the level-0 sites'
+    sscn.LabelScores (`top_k` best classes among them; labels < 0 mark sites
+    without one) and returns (loss, gradients), gradients a dict with any of
+    dlogprob, dentropy, dtop as sscn.label_scores_backward takes them."""
+    if keep not in ("full", "q8"):
+        raise ValueError(f"keep must be 'full' or 'q8', got {keep!r}")
+    if objective is None and top_k:
+        raise ValueError("top_k without an objective")
     channels = P.channels
     L = len(channels)
     if geom.levels != L:
@@ -87,9 +123,10 @@ def train_step(x, labels, geom, P, lr=0.1, momentum=0.9, weight_decay=1e-4, upda
 
     def unit(u, inp):
         e = {"u": u}
-        a = _bn_relu(u.name, inp, P, e)
+        a = _bn_relu(u.name, inp, P, e, keep)
         y = sscn.sparse_conv_forward(a, P.compute[u.name], geom.rulebook(u))
-        e["y"] = y
+        if trace is not None:
+            e["y"] = y
         tape.append(e)
         return y
 
@@ -103,36 +140,41 @@ def train_step(x, labels, geom, P, lr=0.1, momentum=0.9, weight_decay=1e-4, upda
             h = unit(by_name[f"down{l}"], h)
     for l in reversed(range(L - 1)):
         up = unit(by_name[f"up{l}"], h)
-        h = sscn.concat_cols(skips[l], up)
+        h = sscn.concat_cols(skips.pop(l), up)
+        del up
         h = unit(by_name[f"dec{l}a"], h)
         h = unit(by_name[f"dec{l}b"], h)
     head = {}
-    z = _bn_relu("head", h, P, head)
+    z = _bn_relu("head", h, P, head, keep)
     logits = sscn.sparse_conv_forward_ex(z, P.compute["head"], geom.head, bias=P.master["head"][3])
-    loss, dlogits = sscn.softmax_nll(logits, labels)
+    if objective is None:
+        loss, dlogits = sscn.softmax_nll(logits, labels)
+    else:
+        scores = sscn.label_scores(logits, labels, top_k)
+        loss, wanted = objective(scores)
+        dlogits = sscn.label_scores_backward(logits, scores, labels, **wanted)
+    dx = torch.empty_like(h)
+    del h, z, skips  # what the tape does not keep goes now
 
     grads = {}
-    dz, dWh = sscn.sparse_conv_backward(z, P.compute["head"], dlogits, geom.head)
     dbias = sscn.column_sum(dlogits)
-    dx = torch.empty_like(h)
-    dg, db = _bn_relu_back("head", dz, head, P, [(dx, None, None)])
-    grads["head"] = [dg, db, dWh, dbias]
+    dz, grads["head"] = _unit_back("head", dlogits, head, geom.head, P, [(dx, None, None)])
+    grads["head"].append(dbias)
     if trace is not None:
         trace["head"] = dict(head, dy=dlogits, da=dz, dx=dx, logits=logits)
 
     def unit_back(dy, split=None, add=None):
         e = tape.pop()
         u = e["u"]
-        da, dW = sscn.sparse_conv_backward(e["a"], P.compute[u.name], dy, geom.rulebook(u))
+        rb = geom.rulebook(u)
+        new = lambda c: torch.empty((rb.n_in, c), dtype=dy.dtype, device=dy.device)
         if split is None:
-            out = torch.empty_like(e["x"])
-            outs, res = [(out, None, add)], out
+            res = new(u.cin)
+            outs = [(res, None, add)]
         else:
-            res = [torch.empty((e["x"].shape[0], hi - lo), dtype=e["x"].dtype, device=e["x"].device)
-                   for lo, hi in split]
+            res = [new(hi - lo) for lo, hi in split]
             outs = [(r, cols, None) for r, cols in zip(res, split)]
-        dg, db = _bn_relu_back(u.name, da, e, P, outs)
-        grads[u.name] = [dg, db, dW]
+        da, grads[u.name] = _unit_back(u.name, dy, e, rb, P, outs)
         if trace is not None:
             trace[u.name] = dict(e, dy=dy, da=da, dx=res)
         return res

@@ -1,0 +1,338 @@
+"""8-bit activation checkpoints on the GPU against the fp64 oracle.
+
+Codes, exponent bytes, kept values and masks are equal, not near: the oracle
+forms xhat with the same two fp32 roundings.  With u = 2^-24: a column sum is
+fp64 throughout and rounded once (u of it, and what 2^-50 of the summed
+magnitudes adds); restored activations are one fused multiply-add and the
+rounding to the type; dx is a sum of three products whose factors carry up to
+seven roundings, and the type's rounding.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import sscn_oracle as O
+from paper_1711_10275_amd import sscn, train
+from paper_1711_10275_amd import synthetic as S
+from tests.gpu_common import dev, host
+
+pytestmark = pytest.mark.gpu
+
+TD = {"f32": torch.float32, "bf16": torch.bfloat16}
+U = 2.0 ** -24
+
+
+def half_step(dtype):
+    return torch.finfo(TD[dtype]).eps / 2
+
+
+def draw(n, c, dtype, seed):
+    rng = np.random.default_rng(seed)
+    x = (rng.standard_normal((n, c)) * 2 + rng.normal(0, 2, c)).astype(np.float32)
+    x[:, ::7] *= 1e-3
+    x[rng.random(n) < 0.05] *= 50
+    gamma = rng.normal(0, 1, c).astype(np.float32)
+    gamma[::5] = np.abs(gamma[::5])
+    if c > 2:
+        gamma[c // 2] = 0.0
+    beta = rng.normal(0, 0.7, c).astype(np.float32)
+    return (S.bf16_round(x) if dtype == "bf16" else x), gamma, beta
+
+
+def strided(a, dtype, pad):
+    t = dev(a, TD[dtype])
+    if not pad:
+        return t
+    wide = torch.full((a.shape[0], a.shape[1] + pad), float("nan"), dtype=t.dtype, device=t.device)
+    wide[:, :a.shape[1]] = t
+    return wide[:, :a.shape[1]]
+
+
+def stats_of(t, gamma, beta):
+    st = sscn.batchnorm_forward(t, dev(gamma), dev(beta))
+    return st, [host(v) for v in (st.mean, st.invstd, st.scale)]
+
+
+def check_keep(x, gamma, beta, dtype, pad=0):
+    t = strided(x, dtype, pad)
+    st, (mean, invstd, scale) = stats_of(t, gamma, beta)
+    a, q8 = sscn.batchnorm_relu_apply_q8(t, st, dev(gamma), dev(beta))
+    assert torch.equal(a, sscn.batchnorm_relu_apply(t, st, dev(beta)))
+    codes, exps = O.q8_encode(x, mean, invstd, scale, gamma, beta)
+    np.testing.assert_array_equal(host(q8.exponents), exps)
+    np.testing.assert_array_equal(host(q8.codes), codes)
+    v = O.q8_values(codes, exps)
+    for kind in TD.values():
+        np.testing.assert_array_equal(host(sscn.q8_values(q8, kind)), v)
+    return q8, codes, exps, invstd
+
+
+def check_back(x, gamma, beta, dtype, q8, codes, exps, invstd, pad=0, split=None, seed=1):
+    rng = np.random.default_rng(seed)
+    n, c = x.shape
+    dA = rng.standard_normal((n, c)).astype(np.float32)
+    dA = S.bf16_round(dA) if dtype == "bf16" else dA
+    tA, tg, tb = strided(dA, dtype, pad), dev(gamma), dev(beta)
+    a, dX, dg, db = O.batch_norm_relu_backward_q8(dA, codes, exps, gamma, beta, invstd)
+    got_g, got_b, got_a = sscn.batchnorm_relu_backward_params_q8(tA, q8, tg, tb, restore=True)
+    v = np.abs(O.q8_values(codes, exps))
+    big = np.abs(dA).astype(np.float64)
+    assert (np.abs(host(got_b) - db) <= U * np.abs(db) + 2.0 ** -50 * n * big.sum(0)).all()
+    assert (np.abs(host(got_g) - dg) <= U * np.abs(dg) + 2.0 ** -50 * n * (big * v).sum(0)).all()
+    err = np.abs(host(got_a) - a)
+    assert (err <= (U + half_step(dtype)) * np.abs(a) * (1 + 1e-6) + 1e-44).all()
+    again = sscn.batchnorm_relu_backward_params_q8(tA, q8, tg, tb)
+    assert again[2] is None and torch.equal(again[0], got_g) and torch.equal(again[1], got_b)
+    gi = np.abs(gamma.astype(np.float64) * invstd)
+    size = gi * (big + np.abs(db) / n + v * np.abs(dg) / n)
+    for lo, hi in split or [(0, c)]:
+        add = rng.standard_normal((n, hi - lo)).astype(np.float32) if split else None
+        if add is not None and dtype == "bf16":
+            add = S.bf16_round(add)
+        want = dX[:, lo:hi] + (add if add is not None else 0.0)
+        out = strided(np.zeros((n, hi - lo), np.float32), dtype, pad)
+        got = sscn.batchnorm_relu_backward_input_q8(tA, q8, tg, tb, dev(invstd), got_g, got_b, out,
+                                                    add=strided(add, dtype, pad) if add is not None else None,
+                                                    cols=(lo, hi) if split else None)
+        b = 9 * U * size[:, lo:hi] + U * np.abs(want)
+        b = b + half_step(dtype) * (np.abs(want) + b)
+        err = np.abs(host(got) - want)
+        assert (err <= b).all(), f"dx worst {np.max(err / b):.3g} of its bound"
+        if pad:
+            assert torch.isnan(got._base[:, hi - lo:]).all()
+
+
+SIZES = [(1, 1), (2, 32), (777, 5), (1799, 16), (300, 31), (301, 33), (5000, 64), (4001, 70), (999, 96), (513, 128),
+         (257, 160), (100, 255), (65, 256), (130, 512), (40, 513), (9, 1000), (70001, 32)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,c", SIZES)
+def test_keep_and_backward(n, c, dtype):
+    x, gamma, beta = draw(n, c, dtype, n + c)
+    check_back(x, gamma, beta, dtype, *check_keep(x, gamma, beta, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad", [1, 3, 16])
+@pytest.mark.parametrize("n,c", [(1, 32), (401, 16), (300, 32), (200, 70), (130, 128), (50, 520)])
+def test_strided_rows(n, c, pad, dtype):
+    x, gamma, beta = draw(n, c, dtype, n + c + pad)
+    check_back(x, gamma, beta, dtype, *check_keep(x, gamma, beta, dtype, pad), pad=pad)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c,ranges", [(64, [(0, 32), (32, 64)]), (70, [(0, 35), (35, 70)]), (48, [(0, 24), (24, 48)]),
+                                      (256, [(0, 128), (128, 256)]), (33, [(0, 1), (1, 33), (32, 33)])])
+def test_column_ranges_with_another_gradient(c, ranges, dtype):
+    x, gamma, beta = draw(400, c, dtype, c)
+    check_back(x, gamma, beta, dtype, *check_keep(x, gamma, beta, dtype), split=ranges)
+
+
+def test_codes_cut_the_relu_where_the_forward_did():
+    """Values around the border of the ReLU, many to a step of their block."""
+    rng = np.random.default_rng(4)
+    n, c = 4000, 64
+    gamma = np.where(rng.random(c) < 0.5, 1, -1).astype(np.float32) * rng.uniform(0.5, 2, c).astype(np.float32)
+    beta = rng.normal(0, 1, c).astype(np.float32)
+    x = (-beta / gamma + rng.normal(0, 1e-3, (n, c))).astype(np.float32)
+    x[:, 0] = 100
+    x[:, 32] = 3
+    t = dev(x)
+    st, (mean, invstd, scale) = stats_of(t, gamma, beta)
+    a, q8 = sscn.batchnorm_relu_apply_q8(t, st, dev(gamma), dev(beta))
+    _, _, back = sscn.batchnorm_relu_backward_params_q8(t, q8, dev(gamma), dev(beta), restore=True)
+    assert torch.equal(a > 0, back > 0) and 0.2 < (a > 0).float().mean() < 0.8
+
+
+def test_values_that_are_not_finite():
+    x, gamma, beta = draw(40, 70, "f32", 6)
+    t = dev(x)
+    st, _ = stats_of(t, gamma, beta)
+    t[3, 5], t[7, 40], t[9, 69] = float("nan"), float("inf"), -float("inf")
+    a, q8 = sscn.batchnorm_relu_apply_q8(t, st, dev(gamma), dev(beta))
+    bad = np.zeros((40, 3), bool)
+    bad[3, 0] = bad[7, 1] = bad[9, 2] = True
+    np.testing.assert_array_equal(host(q8.exponents) == 255, bad)
+    gone = torch.from_numpy(np.repeat(bad, 32, 1)[:, :70].copy()).to(t.device)
+    for kind in TD.values():
+        assert torch.equal(torch.isnan(sscn.q8_values(q8, kind)), gone)
+    dA = torch.ones_like(t)
+    dg, db, back = sscn.batchnorm_relu_backward_params_q8(dA, q8, dev(gamma), dev(beta), restore=True)
+    assert torch.equal(torch.isnan(back), gone)
+    assert torch.isnan(dg).sum() == 70      # every block of 32 holds one: no channel's sum is left whole
+    assert torch.isfinite(db).all()         # masked, so dbeta does not see them
+
+
+def test_no_rows():
+    q8 = sscn.Q8(torch.empty((0, 40), dtype=torch.int8, device="cuda:0"),
+                 torch.empty((0, 2), dtype=torch.uint8, device="cuda:0"))
+    one, dA = torch.ones(40, device="cuda:0"), torch.empty((0, 40), device="cuda:0")
+    dg, db, a = sscn.batchnorm_relu_backward_params_q8(dA, q8, one, one, restore=True)
+    assert (dg == 0).all() and (db == 0).all() and a.shape == (0, 40)
+    assert sscn.q8_values(q8).shape == (0, 40)
+    sscn.batchnorm_relu_backward_input_q8(dA, q8, one, one, one, dg, db, torch.empty_like(dA))
+
+
+def test_in_place_and_reused_buffers():
+    """y may be x, and dx may be the gradient added to it."""
+    x, gamma, beta = draw(500, 48, "f32", 8)
+    t = dev(x)
+    st, _ = stats_of(t, gamma, beta)
+    a, q8 = sscn.batchnorm_relu_apply_q8(t, st, dev(gamma), dev(beta))
+    a2, q2 = sscn.batchnorm_relu_apply_q8(t, st, dev(gamma), dev(beta), out=t)
+    assert a2 is t and torch.equal(a, t) and torch.equal(q8.codes, q2.codes) and torch.equal(q8.exponents, q2.exponents)
+    dA, add = torch.randn_like(a), torch.randn_like(a)
+    dg, db, _ = sscn.batchnorm_relu_backward_params_q8(dA, q8, dev(gamma), dev(beta))
+    args = (dA, q8, dev(gamma), dev(beta), st.invstd, dg, db)
+    want = sscn.batchnorm_relu_backward_input_q8(*args, torch.empty_like(a), add=add)
+    assert torch.equal(sscn.batchnorm_relu_backward_input_q8(*args, add, add=add), want)
+
+
+@pytest.mark.parametrize("c", [32, 70])
+def test_graphs_and_streams(c):
+    x, gamma, beta = draw(3000, c, "f32", 10)
+    t, tg, tb = dev(x), dev(gamma), dev(beta)
+    st, _ = stats_of(t, gamma, beta)
+    dA = torch.randn_like(t)
+
+    def calls():
+        a, q8 = sscn.batchnorm_relu_apply_q8(t, st, tg, tb)
+        dg, db, back = sscn.batchnorm_relu_backward_params_q8(dA, q8, tg, tb, restore=True)
+        dx = sscn.batchnorm_relu_backward_input_q8(dA, q8, tg, tb, st.invstd, dg, db, torch.empty_like(t))
+        return a, q8.codes, q8.exponents, sscn.q8_values(q8), dg, db, back, dx
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        on_side = calls()
+    torch.cuda.current_stream().wait_stream(side)
+    for a, b in zip(on_side, calls()):
+        assert torch.equal(a, b)
+    graphs = []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = calls()
+        graphs.append((g, out))
+    for turn in range(3):
+        t.copy_(dev(draw(3000, c, "f32", 30 + turn)[0]))
+        for g, _ in graphs:
+            g.replay()
+        want = calls()
+        torch.cuda.synchronize()
+        for _, out in graphs:
+            for a, b in zip(out, want):
+                assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------ a training step
+CH, NCLS = (8, 16, 24), 6
+
+
+def _step(dtype, **more):
+    coords = S.scenes_small(batch=2, L=32, target_per_sample=3000)
+    n = coords.shape[0]
+    X = S.features(n, CH[0], S.SEED_FEAT + 41, bf16=dtype == "bf16")
+    lab = S.labels(n, NCLS, 42)
+    geom = train.Geometry(dev(coords), (32, 32, 32), levels=len(CH))
+    P = train.Params(CH, NCLS, S.train_params, dtype=TD[dtype])
+    return train.train_step(dev(X, TD[dtype]), more.pop("labels", dev(lab)), geom, P, update=False, **more), lab
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_train_step_with_kept_codes(dtype):
+    """The loss is that of the step that keeps everything, bit for bit (the
+    forward does not read the codes); every unit, fed its own tensors, matches
+    the oracle's backward pass from its codes."""
+    (loss, grads), _ = _step(dtype)
+    trace = {}
+    (loss8, grads8), _ = _step(dtype, keep="q8", trace=trace)
+    assert torch.equal(loss, loss8) and set(grads) == set(grads8) == set(trace)
+    draw_ = {name: S.train_params(name, g[2].shape[0], g[2].shape[1], g[2].shape[2]) for name, g in grads8.items()}
+    for name, e in trace.items():
+        gamma, beta = draw_[name][0], draw_[name][1]
+        codes, exps, invstd = host(e["q8"].codes), host(e["q8"].exponents), host(e["st"].invstd)
+        a, dX, dg, db = O.batch_norm_relu_backward_q8(host(e["da"]), codes, exps, gamma, beta, invstd)
+        n = codes.shape[0]
+        big, v = np.abs(host(e["da"])).astype(np.float64), np.abs(O.q8_values(codes, exps))
+        assert (np.abs(host(e["a"]) - a) <= (U + half_step(dtype)) * np.abs(a) * (1 + 1e-6)).all(), name
+        assert (np.abs(host(grads8[name][0]) - dg) <= U * np.abs(dg) + 2.0 ** -50 * n * (big * v).sum(0)).all(), name
+        assert (np.abs(host(grads8[name][1]) - db) <= U * np.abs(db) + 2.0 ** -50 * n * big.sum(0)).all(), name
+        dxs = e["dx"] if isinstance(e["dx"], list) else [e["dx"]]
+        if name.startswith("down"):
+            dX = dX + host(trace[f"dec{name[4:]}a"]["dx"][0])
+        gi = np.abs(gamma.astype(np.float64) * invstd)
+        b = 9 * U * gi * (big + np.abs(db) / n + v * np.abs(dg) / n) + U * np.abs(dX)
+        b = b + half_step(dtype) * (np.abs(dX) + b)
+        assert (np.abs(np.concatenate([host(t) for t in dxs], 1) - dX) <= b).all(), name
+    # the head's gradients see exact codes only through a: bias alone is untouched
+    assert torch.equal(grads["head"][3], grads8["head"][3])
+    for name in grads:      # and the whole gradient keeps its direction
+        x, y = host(grads[name][2]).ravel(), host(grads8[name][2]).ravel()
+        assert x @ y > 0.98 * np.linalg.norm(x) * np.linalg.norm(y), name
+
+
+def test_train_step_tape_is_smaller():
+    """Peak memory of a step on kept codes, over what is there before it."""
+    coords = S.scenes_small(batch=2, L=64, target_per_sample=20000)
+    geom = train.Geometry(dev(coords), (64, 64, 64), levels=2)
+    P = train.Params((64, 64), NCLS, S.train_params)
+    x, lab = dev(S.features(coords.shape[0], 64, 1)), dev(S.labels(coords.shape[0], NCLS, 2))
+    peak = {}
+    for keep in ("full", "q8"):
+        for _ in range(2):
+            torch.cuda.synchronize()
+            base = torch.cuda.memory_allocated()
+            torch.cuda.reset_peak_memory_stats()
+            train.train_step(x, lab, geom, P, update=False, keep=keep)
+            torch.cuda.synchronize()
+            peak[keep] = torch.cuda.max_memory_allocated() - base
+    assert peak["q8"] < 0.6 * peak["full"], peak
+
+
+@pytest.mark.parametrize("keep", ["full", "q8"])
+def test_train_step_with_an_objective(keep):
+    """Mean over the labelled sites, an entropy term and the best classes: the
+    logits' gradient that the step uses is the oracle's, and with every site
+    labelled and nothing else it is softmax_nll's."""
+    seen = {}
+
+    def objective(s):
+        n = s.entropy.shape[0]
+        has = (lab_t >= 0).float()
+        w = -has / has.sum()
+        seen.update(scores=s, w=w)
+        dtop = torch.full((n, 2), -0.01 / n, device=w.device)
+        return (w * s.logprob).sum(), dict(dlogprob=w, dentropy=torch.full((n,), 0.1 / n, device=w.device), dtop=dtop)
+
+    n = S.scenes_small(batch=2, L=32, target_per_sample=3000).shape[0]
+    lab = S.labels(n, NCLS, 42)
+    lab[::3] = -1
+    lab_t = dev(lab)
+    trace = {}
+    (loss, grads), _ = _step("f32", labels=lab_t, keep=keep, objective=objective, top_k=2, trace=trace)
+    z = host(trace["head"]["logits"])
+    lp, H, _, top, _ = O.label_scores(z, lab, 2)
+    has = lab >= 0
+    assert abs(float(loss) + lp[has].mean()) < 1e-5
+    want = O.label_scores_backward(z, lab, np.where(has, -1 / has.sum(), 0), np.full(n, 0.1 / n), top, np.full((n, 2), -0.01 / n))
+    got = host(trace["head"]["dy"])
+    assert np.abs(got - want).max() < 1e-5 * np.abs(want).max()
+    assert all(torch.isfinite(t).all() for g in grads.values() for t in g)
+    # the plain mean, both ways
+    lab2 = dev(S.labels(n, NCLS, 42))
+    (loss1, grads1), _ = _step("f32", labels=lab2)
+    mean = torch.full((n,), -1.0 / n, device=lab2.device)
+    (loss2, grads2), _ = _step("f32", labels=lab2, objective=lambda s: ((mean * s.logprob).sum(), dict(dlogprob=mean)))
+    assert abs(float(loss1) - float(loss2)) < 1e-5 * abs(float(loss1))
+    for name in grads1:
+        for a, b in zip(grads1[name], grads2[name]):
+            assert float((a - b).norm()) <= 2e-5 * float(a.norm()) + 1e-9, name
+
+
+def test_train_step_refuses_what_it_does_not_know():
+    with pytest.raises(ValueError, match="keep"):
+        _step("f32", keep="fp8")
+    with pytest.raises(ValueError, match="top_k"):
+        _step("f32", top_k=2)
