@@ -12,6 +12,7 @@
 
 #include "internal.h"
 #include "numeric.h"
+#include "wave.h"
 
 namespace sscn {
 
@@ -34,81 +35,6 @@ struct RowSums {
   float s, a;
   int eq;
 };
-__device__ __forceinline__ void add_value(RowSums& q, float x, float m, float base) {
-  const float d = x - base;
-  const float e = expf(d);
-  const bool top = x == m;
-  q.s += top ? 0.f : e;  // a NaN stays in s
-  q.eq += top;
-  q.a += e * (d < -200.f ? -200.f : d);  // exp(-200) is 0: no 0 * inf
-}
-// (L, H) from the sums.  A row of -inf only: 0, 0.  NaN or +inf in the row: NaN.
-__device__ __forceinline__ float2 finish(float m, const RowSums& q) {
-  if (m == INFINITY || q.s != q.s) return make_float2(NAN, NAN);
-  if (m == -INFINITY) return make_float2(0.f, 0.f);
-  const float t = q.s + (float)(q.eq - 1);
-  const float l = log1pf(t);
-  return make_float2(l, l - q.a / (1.f + t));
-}
-
-__device__ __forceinline__ uint64_t shfl_xor_u64(uint64_t v, int d) {
-  const uint32_t lo = __shfl_xor((uint32_t)v, d, 64), hi = __shfl_xor((uint32_t)(v >> 32), d, 64);
-  return (uint64_t)hi << 32 | lo;
-}
-
-// One wavefront per row, lanes over the classes; the best classes by one more
-// pass over the row for each.
-template <typename T>
-__global__ __launch_bounds__(256) void k_scores(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
-                                                const int32_t* __restrict__ labels, int top_k,
-                                                float* __restrict__ logprob, float* __restrict__ entropy,
-                                                float* __restrict__ stats, int32_t* __restrict__ top_index,
-                                                float* __restrict__ top_logprob) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int64_t r = (int64_t)blockIdx.x * 4 + wave; r < n; r += (int64_t)gridDim.x * 4) {
-    const T* row = z + r * ldz;
-    float m = -INFINITY;
-    for (int k = lane; k < classes; k += 64) m = fmaxf(m, ld(row + k));
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-    const float base = m == -INFINITY ? 0.f : m;
-    RowSums q{0.f, 0.f, 0};
-    for (int k = lane; k < classes; k += 64) add_value(q, ld(row + k), m, base);
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) {
-      q.s += __shfl_xor(q.s, d, 64);
-      q.a += __shfl_xor(q.a, d, 64);
-      q.eq += __shfl_xor(q.eq, d, 64);
-    }
-    const float2 lh = finish(m, q);
-    uint64_t last = ~0ull;
-    for (int j = 0; j < top_k; ++j) {
-      uint64_t best = 0;
-      for (int k = lane; k < classes; k += 64) {
-        const uint64_t key = rank_key(ld(row + k), (uint32_t)k);
-        if (key < last && key > best) best = key;
-      }
-#pragma unroll
-      for (int d = 32; d >= 1; d >>= 1) best = max(best, shfl_xor_u64(best, d));
-      last = best;
-      if (lane == 0) {
-        const uint32_t k = key_class(best);
-        top_index[r * top_k + j] = (int32_t)k;
-        top_logprob[r * top_k + j] = (ld(row + k) - base) - lh.x;
-      }
-    }
-    if (lane == 0) {
-      if (logprob) {
-        const int lab = labels[r];
-        logprob[r] = lab < 0 ? 0.f : lab >= classes ? NAN : (ld(row + lab) - base) - lh.x;
-      }
-      entropy[r] = lh.y;
-      stats[2 * r] = m;
-      stats[2 * r + 1] = lh.x;
-    }
-  }
-}
-
 // The gradient.  With A_k what class k receives directly (g = dlogprob where k
 // is the label, dtop_j where k is the j-th best class) and G their sum,
 //   dx_k = -A_k expm1(log p_k) - p_k ((G - A_k) + h (log p_k + H)),  h = dentropy,
@@ -147,6 +73,381 @@ __global__ __launch_bounds__(256) void k_scores_grad(const T* __restrict__ z, in
   }
 }
 
+// ------------------------------------------------------------- longer rows
+// A row is read as 16-byte (W = 1: 4-byte) pieces at their own alignment, so
+// that rows that start anywhere are read wide; the pieces at its ends that it
+// shares with its neighbours are read value by value. A workgroup of W
+// wavefronts holds a chunk of 64 W E values in registers, E a thread: one read
+// of the logits, the maximum before the exponentials.
+template <typename T, int W, int E>
+struct Chunk {
+  static constexpr int V = (W == 1 ? 4 : 16) / (int)sizeof(T);  // values per piece
+  static constexpr int G = E / V;                               // pieces per thread
+  static constexpr int kThreads = 64 * W;
+  static constexpr int64_t kPieces = (int64_t)kThreads * G;     // per chunk
+
+  // Class of value i of piece g of this thread, for the chunk that starts at class c0.
+  __device__ static int cls(int64_t c0, int g, int i) {
+    return (int)(c0 + ((int64_t)g * kThreads + threadIdx.x) * V + i);
+  }
+  // Classes between the first whole piece's alignment and the row's start.
+  __device__ static int head(const T* row) { return (int)(reinterpret_cast<uintptr_t>(row) % (V * sizeof(T)) / sizeof(T)); }
+
+  __device__ static void unpack(const T* piece, float (&x)[V]) {
+    if constexpr (V == 1) {
+      x[0] = ld(piece);
+    } else if constexpr (sizeof(T) == 4) {
+      const float4 q = *reinterpret_cast<const float4*>(piece);
+      x[0] = q.x; x[1] = q.y; x[2] = q.z; x[3] = q.w;
+    } else {
+      uint32_t w[V / 2];
+      if constexpr (V == 2) {
+        w[0] = *reinterpret_cast<const uint32_t*>(piece);
+      } else {
+        const uint4 q = *reinterpret_cast<const uint4*>(piece);
+        w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+      }
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      }
+    }
+  }
+  // The chunk's values; -inf past the row's ends.  c0 = -head + chunk * kPieces * V.
+  __device__ static void load(const T* row, int classes, int64_t c0, float (&x)[G][V]) {
+    const int64_t wave0 = c0 + (int64_t)(threadIdx.x & ~63) * V;  // first class of this wavefront's first piece
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const int64_t first = wave0 + (int64_t)g * kThreads * V;    // uniform in the wavefront
+      if (first >= 0 && first + 64 * V <= classes) {
+        unpack(row + (first + (int64_t)(threadIdx.x & 63) * V), x[g]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const int64_t k = first + (int64_t)(threadIdx.x & 63) * V + i;
+          x[g][i] = k >= 0 && k < classes ? ld(row + k) : -INFINITY;
+        }
+      }
+    }
+  }
+};
+
+// What one chunk (or several joined) says of a row: m, t = sum of exp(x - m)
+// but one largest, a = sum of exp(x - m) (x - m).
+struct Part {
+  float m, t, a;
+};
+__device__ __forceinline__ Part join(const Part& p, const Part& q) {
+  const bool first = p.m >= q.m;
+  const Part &hi = first ? p : q, &lo = first ? q : p;
+  if (lo.m == -INFINITY) return {OpMax::of(p.m, q.m), hi.t, hi.a};
+  const float d = lo.m - hi.m, e = expf(d);
+  // the low part's values, its largest among them, shift by d
+  return {OpMax::of(p.m, q.m), hi.t + e * (1.f + lo.t), hi.a + e * (lo.a + (d < -200.f ? -200.f : d) * (1.f + lo.t))};
+}
+__device__ __forceinline__ float2 finish(const Part& p) {
+  if (p.m == INFINITY || p.m != p.m) return make_float2(NAN, NAN);
+  if (p.m == -INFINITY) return make_float2(0.f, 0.f);
+  const float l = log1pf(p.t);
+  return make_float2(l, l - p.a / (1.f + p.t));
+}
+
+struct Outputs {
+  float *logprob, *entropy, *stats;
+  int32_t* top_index;
+  float* top_logprob;
+};
+
+// Writes row r.  top: top_k keys in LDS, best first, 0 where the row has fewer
+// classes above -inf: the lowest of the others follow.
+template <typename T>
+__device__ __forceinline__ void write_row(const T* row, int64_t r, int classes, const int32_t* labels, int top_k,
+                                          const Part& p, uint64_t* top, const Outputs& o) {
+  const int lane = threadIdx.x & 63;
+  const float2 lh = finish(p);
+  const float base = p.m == -INFINITY ? 0.f : p.m;
+  if (top_k > 0 && lane == 0 && top[top_k - 1] == 0) {
+    int have = 0;
+    while (top[have] != 0) ++have;
+    uint32_t k = 0;
+    for (int j = have; j < top_k; ++k) {
+      bool listed = false;
+      for (int i = 0; i < have; ++i) listed |= key_class(top[i]) == k;
+      if (!listed) top[j++] = rank_key(-INFINITY, k);
+    }
+  }
+  if (lane == 0) {
+    if (o.logprob) {
+      const int lab = labels[r];
+      o.logprob[r] = lab < 0 ? 0.f : lab >= classes ? NAN : (ld(row + lab) - base) - lh.x;
+    }
+    o.entropy[r] = lh.y;
+    o.stats[2 * r] = p.m;
+    o.stats[2 * r + 1] = lh.x;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (lane < top_k) {
+    const uint32_t k = key_class(top[lane]);
+    o.top_index[r * top_k + lane] = (int32_t)k;
+    o.top_logprob[r * top_k + lane] = (ld(row + k) - base) - lh.x;
+  }
+}
+
+// One chunk of one row per turn of a workgroup; `parts` chunks per row.  With
+// one the row is written, with more its Part and its best keys are left for
+// k_scores_join.
+//
+// The best classes: T, the least of at least top_k groups' maxima (groups of
+// threads that share no value), is no larger than the top_k-th best value, so
+// what is below T is out.  Few values are left (about top_k log(top_k) of
+// unordered ones); each counts the keys above its own, which is its rank.
+// Values of -inf stay out of the lists.  A list that overflows (ties at T), or
+// a NaN, takes the slow way: one more pass over the registers per class.
+template <typename T, int W, int E>
+__global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
+                                                         int parts, const int32_t* __restrict__ labels, int top_k,
+                                                         Outputs o, float4* __restrict__ part_out,
+                                                         uint64_t* __restrict__ keys_out) {
+  using C = Chunk<T, W, E>;
+  constexpr int kList = 64 * W * E < 2048 ? 64 * W * E : 2048;
+  __shared__ uint64_t list[kList], top[kMaxTop];
+  __shared__ float red[3][W];
+  __shared__ int count, ties[W];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t total = n * parts;
+  for (int64_t item = blockIdx.x; item < total; item += gridDim.x) {
+    const int64_t r = item / parts;
+    const T* row = z + r * ldz;
+    const int64_t c0 = (item - r * parts) * C::kPieces * C::V - C::head(row);
+    float x[C::G][C::V];
+    C::load(row, classes, c0, x);
+    float own = -INFINITY;  // this thread's maximum
+#pragma unroll
+    for (int g = 0; g < C::G; ++g)
+#pragma unroll
+      for (int i = 0; i < C::V; ++i) own = OpMax::of(own, x[g][i]);
+    // maxima of groups of lanes, and the threshold from them
+    const float v4 = wave_reduce<OpMax, 1, 4>(own), v8 = wave_reduce<OpMax, 4, 8>(v4);
+    const float v16 = wave_reduce<OpMax, 8, 16>(v8), v32 = wave_reduce<OpMax, 16, 32>(v16);
+    float m = wave_reduce<OpMax, 32, 64>(v32), cut = m;
+    if constexpr (W == 1) {
+      if (top_k > 1) cut = wave_reduce<OpMin>(top_k <= 2 ? v32 : top_k <= 4 ? v16 : top_k <= 8 ? v8 : v4);
+    } else {
+      static_assert(W == 4);
+      if (top_k > 4) cut = wave_reduce<OpMin>(top_k <= 8 ? v32 : v16);
+    }
+    if (threadIdx.x == 0) count = 0;
+    if (threadIdx.x < kMaxTop) top[threadIdx.x] = 0;
+    if constexpr (W > 1) {
+      if (lane == 0) {
+        red[0][wave] = m;
+        red[1][wave] = cut;
+      }
+    }
+    __syncthreads();
+    if constexpr (W > 1) {
+      const float m0 = red[0][0], m1 = red[0][1], m2 = red[0][2], m3 = red[0][3];
+      m = OpMax::of(OpMax::of(m0, m1), OpMax::of(m2, m3));
+      const float least = fminf(fminf(red[1][0], red[1][1]), fminf(red[1][2], red[1][3]));
+      // of four maxima the first, second, third or fourth largest
+      const float hi0 = fmaxf(m0, m1), lo0 = fminf(m0, m1), hi1 = fmaxf(m2, m3), lo1 = fminf(m2, m3);
+      const float mid0 = fminf(hi0, hi1), mid1 = fmaxf(lo0, lo1);
+      cut = top_k == 1 ? m : top_k == 2 ? fmaxf(mid0, mid1) : top_k == 3 ? fminf(mid0, mid1) : least;
+    }
+    if (top_k > 0 && m == m) {
+#pragma unroll
+      for (int g = 0; g < C::G; ++g)
+#pragma unroll
+        for (int i = 0; i < C::V; ++i)
+          if (x[g][i] >= cut && x[g][i] > -INFINITY) {
+            const int at = atomicAdd(&count, 1);
+            if (at < kList) list[at] = rank_key(x[g][i], (uint32_t)C::cls(c0, g, i));
+          }
+    }
+    // the sums, of 2^h with h = (x - m) log2(e): the largest are counted and
+    // left out.  h is one rounded product: a term is off by up to 2.25 |x - m|
+    // half steps, which its own size e^(x - m) outweighs; forming the product's
+    // low part too would cost three more operations a value.
+    RowSums q{0.f, 0.f, 0};
+    float y[C::G][C::V];
+#pragma unroll
+    for (int g = 0; g < C::G; ++g)
+#pragma unroll
+      for (int i = 0; i < C::V; ++i) y[g][i] = x[g][i];
+    if (own == m) {
+#pragma unroll
+      for (int g = 0; g < C::G; ++g)
+#pragma unroll
+        for (int i = 0; i < C::V; ++i)
+          if (y[g][i] == m) {
+            y[g][i] = -INFINITY;
+            ++q.eq;
+          }
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int g = 0; g < C::G; ++g)
+#pragma unroll
+      for (int i = 0; i < C::V; ++i) {
+        const float h = fmaxf((y[g][i] - base) * 1.44269504088896340736f, -300.f);  // 2^-300 is 0
+        const float e = __builtin_amdgcn_exp2f(h);
+        q.s += e;
+        q.a = fmaf(e, h, q.a);
+      }
+    q.s = wave_reduce<OpAdd>(q.s);
+    q.a = wave_reduce<OpAdd>(q.a) * 0.69314718055994530942f;
+    q.eq = (int)wave_reduce<OpAdd>((float)q.eq);  // at most 8192: exact
+    if constexpr (W > 1) {
+      if (lane == 0) {
+        red[2][wave] = q.s;
+        ties[wave] = q.eq;
+      }
+      __syncthreads();  // also: every wavefront has read red[0] and red[1]
+      if (lane == 0) red[1][wave] = q.a;
+      q.s = (red[2][0] + red[2][1]) + (red[2][2] + red[2][3]);
+      q.eq = (ties[0] + ties[1]) + (ties[2] + ties[3]);
+    }
+    __syncthreads();
+    if constexpr (W > 1) q.a = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+    const int found = count;
+    if (top_k > 0) {
+      if (m != m || found > kList) {
+        uint64_t last = ~0ull;
+        for (int j = 0; j < top_k; ++j) {
+          uint64_t best = 0;
+#pragma unroll
+          for (int g = 0; g < C::G; ++g)
+#pragma unroll
+            for (int i = 0; i < C::V; ++i) {
+              const uint64_t key = rank_key(x[g][i], (uint32_t)C::cls(c0, g, i));
+              if (!(x[g][i] == -INFINITY) && key < last && key > best) best = key;
+            }
+          best = wave_max_key(best);
+          if constexpr (W > 1) {
+            __syncthreads();
+            if (lane == 0) list[wave] = best;
+            __syncthreads();
+            best = max(max(list[0], list[1]), max(list[2], list[3]));
+          }
+          last = best;
+          if (threadIdx.x == 0) top[j] = best;
+        }
+      } else {
+        for (int i = threadIdx.x; i < found; i += C::kThreads) {
+          const uint64_t own_key = list[i];
+          int above = 0;
+          for (int j = 0; j < found; ++j) above += list[j] > own_key;
+          if (above < top_k) top[above] = own_key;
+        }
+      }
+      __syncthreads();
+    }
+    const Part p{m, m == -INFINITY ? 0.f : q.s + (float)(q.eq - 1), q.a};
+    if (wave == 0) {
+      if (parts == 1) {
+        write_row(row, r, classes, labels, top_k, p, top, o);
+      } else {
+        if (lane == 0) part_out[item] = make_float4(p.m, p.t, p.a, 0.f);
+        if (lane < top_k) keys_out[item * top_k + lane] = top[lane];
+      }
+    }
+    __syncthreads();  // the next turn writes the LDS again
+  }
+}
+
+// Joins the parts of a row, one wavefront per row.  Lane l takes the parts l,
+// l + 64, ..; the best classes come off the heads of 63 of the parts' lists at
+// a time and of the list so far (lane 63).
+template <typename T>
+__global__ __launch_bounds__(64) void k_scores_join(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
+                                                    int parts, const int32_t* __restrict__ labels, int top_k,
+                                                    Outputs o, const float4* __restrict__ part_in,
+                                                    const uint64_t* __restrict__ keys_in) {
+  __shared__ uint64_t top[kMaxTop];
+  const int lane = threadIdx.x;
+  for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
+    Part p{-INFINITY, 0.f, 0.f};
+    for (int c = lane; c < parts; c += 64) {
+      const float4 q = part_in[r * parts + c];
+      p = join(p, Part{q.x, q.y, q.z});
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const Part q{__shfl_xor(p.m, d, 64), __shfl_xor(p.t, d, 64), __shfl_xor(p.a, d, 64)};
+      p = (lane & d) ? join(q, p) : join(p, q);  // the lower lane's part first: every lane the same
+    }
+    if (lane < kMaxTop) top[lane] = 0;
+    __syncthreads();
+    if (top_k > 0) {
+      for (int c0 = 0; c0 < parts; c0 += 63) {
+        const uint64_t* mine = keys_in + (r * parts + c0 + lane) * top_k;
+        const bool have = lane < 63 && c0 + lane < parts;
+        int at = 0;  // entries taken off this lane's list
+        uint64_t keep = lane < top_k ? top[lane] : 0;  // the list so far
+        uint64_t head = have ? mine[0] : lane == 63 ? top[0] : 0;
+        __syncthreads();
+        for (int j = 0; j < top_k; ++j) {
+          const uint64_t win = wave_max_key(head);
+          if (lane == 0) top[j] = win;
+          const bool took = win != 0 && head == win;
+          const bool old = __ballot(took) >> 63 & 1;  // off the list so far
+          if (took) ++at;
+          const int at63 = __shfl(at, 63, 64);
+          const uint64_t next63 = (uint64_t)__shfl((uint32_t)(keep >> 32), at63 & 63, 64) << 32 |
+                                  __shfl((uint32_t)keep, at63 & 63, 64);
+          if (took && have) head = at < top_k ? mine[at] : 0;
+          if (old && lane == 63) head = at63 < top_k ? next63 : 0;
+        }
+        __syncthreads();
+      }
+    }
+    write_row(z + r * ldz, r, classes, labels, top_k, p, top, o);
+    __syncthreads();
+  }
+}
+
+// Which kernel takes a row, by its length alone (and, for rows of several
+// chunks, by how many there are): one workgroup holds up to 64 W E values.
+struct Route {
+  int waves, per_thread;  // W, E
+  int parts;              // chunks of a row
+};
+Route route_of(int64_t n, int classes) {
+  // up to 7 values of the first piece may belong to the row before
+  const int64_t len = (int64_t)classes + 7;
+  if (classes <= 510) return {1, 8, 1};     // 4-byte pieces: at most one such value
+  if (len <= 2048) return {4, 8, 1};
+  if (len <= 8192) return {4, 32, 1};
+  // long rows: chunks of 8192 once they are enough workgroups for 256 CUs,
+  // else four times as many
+  const int64_t big = ceil_div(len, 8192);
+  return n * big >= 512 ? Route{4, 32, (int)big} : Route{4, 8, (int)ceil_div(len, 2048)};
+}
+
+template <typename T>
+sscn_status launch_chunks(const T* z, int64_t ldz, int64_t n, int classes, const int32_t* labels, int top_k,
+                          const Outputs& o, void* workspace, hipStream_t s) {
+  const Route w = route_of(n, classes);
+  const int64_t items = n * w.parts;
+  float4* parts = (float4*)workspace;
+  uint64_t* keys = (uint64_t*)(parts + items);
+  const unsigned g = (unsigned)std::min<int64_t>(items, w.waves == 1 ? 16384 : 8192);
+  if (w.waves == 1)
+    k_scores_chunk<T, 1, 8><<<g, 64, 0, s>>>(z, ldz, n, classes, w.parts, labels, top_k, o, parts, keys);
+  else if (w.per_thread == 8)
+    k_scores_chunk<T, 4, 8><<<g, 256, 0, s>>>(z, ldz, n, classes, w.parts, labels, top_k, o, parts, keys);
+  else
+    k_scores_chunk<T, 4, 32><<<g, 256, 0, s>>>(z, ldz, n, classes, w.parts, labels, top_k, o, parts, keys);
+  SSCN_HIP(hipGetLastError());
+  if (w.parts > 1) {
+    k_scores_join<T><<<(unsigned)std::min<int64_t>(n, 16384), 64, 0, s>>>(z, ldz, n, classes, w.parts, labels, top_k, o,
+                                                                          parts, keys);
+    SSCN_HIP(hipGetLastError());
+  }
+  return SSCN_OK;
+}
+
 sscn_status check_rows(const void* p, int64_t ld, int64_t n, int classes, sscn_dtype dtype) {
   if (dtype != SSCN_F32 && dtype != SSCN_BF16) return fail(SSCN_ERR_INVALID_ARG, "unknown dtype");
   if (n < 0 || classes < 1) return fail(SSCN_ERR_INVALID_ARG, "scores: n must be >= 0 and classes >= 1");
@@ -173,7 +474,8 @@ extern "C" sscn_status sscn_label_scores_workspace(int64_t n, int32_t classes, i
   if (n < 0 || classes < 1) return fail(SSCN_ERR_INVALID_ARG, "scores: n must be >= 0 and classes >= 1");
   SSCN_TRY(check_top(top_k, classes));
   if (!bytes) return fail(SSCN_ERR_INVALID_ARG, "scores: NULL bytes");
-  *bytes = 0;
+  const Route w = route_of(n, classes);
+  *bytes = w.parts > 1 ? n * w.parts * (int64_t)(sizeof(float4) + sizeof(uint64_t) * top_k) : 0;
   return SSCN_OK;
 }
 
@@ -190,17 +492,13 @@ extern "C" sscn_status sscn_label_scores(const void* logits, int64_t ldz, int64_
     return fail(SSCN_ERR_INVALID_ARG, "scores: NULL top_index or top_logprob");
   int64_t need = 0;
   SSCN_TRY(sscn_label_scores_workspace(n, classes, top_k, &need));
-  if (workspace_bytes < need || (need > 0 && !workspace))
-    return fail(SSCN_ERR_INVALID_ARG, "scores: workspace smaller than sscn_label_scores_workspace says");
+  if (workspace_bytes < need || (need > 0 && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 16 != 0)))
+    return fail(SSCN_ERR_INVALID_ARG, "scores: no workspace of the size that ..._workspace says, 16-byte aligned");
   if (n == 0) return SSCN_OK;
-  if (dtype == SSCN_F32)
-    k_scores<float><<<wave_grid(n), 256, 0, stream>>>((const float*)logits, ldz, n, classes, labels, top_k, logprob,
-                                                      entropy, stats, top_index, top_logprob);
-  else
-    k_scores<uint16_t><<<wave_grid(n), 256, 0, stream>>>((const uint16_t*)logits, ldz, n, classes, labels, top_k,
-                                                         logprob, entropy, stats, top_index, top_logprob);
-  SSCN_HIP(hipGetLastError());
-  return SSCN_OK;
+  const Outputs o{logprob, entropy, stats, top_index, top_logprob};
+  return dtype == SSCN_F32
+             ? launch_chunks((const float*)logits, ldz, n, classes, labels, top_k, o, workspace, stream)
+             : launch_chunks((const uint16_t*)logits, ldz, n, classes, labels, top_k, o, workspace, stream);
 }
 
 extern "C" sscn_status sscn_label_scores_backward(const void* logits, int64_t ldz, int64_t n, int32_t classes,

@@ -1,0 +1,73 @@
+// Reductions over the 64 lanes of a wavefront whose result every lane of the
+// group holds, without LDS: exchanges within rows of 16 lanes are data-
+// parallel-primitive moves, those across rows are the lane swaps of gfx950.
+// The order is fixed, so sums are reproducible.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace sscn {
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+constexpr int kQuadXor1 = 0xb1, kQuadXor2 = 0x4e, kMirror8 = 0x141, kMirror16 = 0x140;
+
+struct OpAdd {
+  __device__ static float of(float a, float b) { return a + b; }
+};
+struct OpMax {  // NaN if either is
+  __device__ static float of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+};
+struct OpMin {
+  __device__ static float of(float a, float b) { return fminf(a, b); }
+};
+
+// Over groups of 2 * FROM .. TO lanes, v uniform in groups of FROM lanes before.
+template <class Op, int FROM = 1, int TO = 64>
+__device__ __forceinline__ float wave_reduce(float v) {
+  const auto f = [](uint32_t b) { return __uint_as_float(b); };
+  if constexpr (FROM < 2 && TO >= 2) v = Op::of(v, f(dpp<kQuadXor1>(__float_as_uint(v))));
+  if constexpr (FROM < 4 && TO >= 4) v = Op::of(v, f(dpp<kQuadXor2>(__float_as_uint(v))));
+  if constexpr (FROM < 8 && TO >= 8) v = Op::of(v, f(dpp<kMirror8>(__float_as_uint(v))));
+  if constexpr (FROM < 16 && TO >= 16) v = Op::of(v, f(dpp<kMirror16>(__float_as_uint(v))));
+  if constexpr (FROM < 32 && TO >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = Op::of(f(r[0]), f(r[1]));
+  }
+  if constexpr (FROM < 64 && TO >= 64) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = Op::of(f(r[0]), f(r[1]));
+  }
+  return v;
+}
+
+// The largest of the lanes' 64-bit keys.
+__device__ __forceinline__ uint64_t key_max(uint64_t a, uint32_t lo, uint32_t hi) {
+  const uint64_t b = (uint64_t)hi << 32 | lo;
+  return a > b ? a : b;
+}
+__device__ __forceinline__ uint64_t wave_max_key(uint64_t v) {
+#define SSCN_KEY_STEP(C) v = key_max(v, dpp<C>((uint32_t)v), dpp<C>((uint32_t)(v >> 32)))
+  SSCN_KEY_STEP(kQuadXor1);
+  SSCN_KEY_STEP(kQuadXor2);
+  SSCN_KEY_STEP(kMirror8);
+  SSCN_KEY_STEP(kMirror16);
+#undef SSCN_KEY_STEP
+  {
+    const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
+    v = key_max((uint64_t)hi[0] << 32 | lo[0], lo[1], hi[1]);
+  }
+  {
+    const auto lo = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+    const auto hi = __builtin_amdgcn_permlane32_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
+    v = key_max((uint64_t)hi[0] << 32 | lo[0], lo[1], hi[1]);
+  }
+  return v;
+}
+
+}  // namespace sscn

@@ -2,13 +2,16 @@
 
 Tolerances, u = 2^-24 (half a step of fp32), t = sum of exp(x - max) but one
 largest, w_k = exp(x_k - max):
- - w_k is off by (2 + |d_k|) u of itself (the difference d_k rounded, exp good
-   to 1 ulp); a sum over N terms of at most A additions in a row adds A u.
+ - w_k = 2^(d_k log2 e) is off by (2 + 2.25 |d_k|) u of itself: the difference
+   d_k rounded is |d_k| u in the exponent (in units of e), its product with
+   log2 e rounded another |d_k| u, the constant itself, 1.44269502162933 for
+   1.44269504088896, another 1.34e-8 |d_k| = 0.23 |d_k| u; the power of two is
+   good to 1 ulp; a sum over N terms of at most A additions in a row adds A u.
    Additions in a row: at most 64 where one thread adds a row, else a lane's
    share (classes / 64 at most) and the joins; A = min(classes, 64) + classes / 64 + 24.
  - L = log1p(t): t / (1 + t) times t's error, plus 2 ulp of the function.
  - H = L - sum w d / (1 + t): the same for sum w d, whose terms are off by
-   (4 + |d|) u of themselves.
+   (4 + 2.25 |d|) u of themselves.
  - log p_k = (x_k - max) - L: two roundings and L's error.
  - the gradient: log p is off by the above, p by that times p; each product and
    sum of the formula adds a rounding of its terms; one rounding to the
@@ -77,15 +80,18 @@ def sums(z):
     d = np.where(np.isneginf(z), -1e4, z - np.where(np.isneginf(m), 0.0, m))
     w = np.exp(d)
     k = z.shape[1]
-    return d, w, np.maximum(w.sum(axis=1) - 1, 0), min(k, 64) + k / 64 + 24
+    rest = w.copy()
+    rest[np.arange(len(z)), w.argmax(axis=1)] = 0.0      # t is a sum without the 1: it may be far below it
+    return d, w, rest.sum(axis=1), min(k, 64) + k / 64 + 24
 
 
 def bounds(z):
     d, w, t, A = sums(z)
     wd, wdd = (w * np.abs(d)).sum(1), (w * d * d).sum(1)
     L = np.log1p(t)
-    bL = U * (((A + 2) * t + wd) / (1 + t) + 4 * L)
-    bH = bL + U * ((A + 6) * wd + wdd + wd * ((A + 2) * t + wd) / (1 + t)) / (1 + t) + 2 * U * (L + wd / (1 + t))
+    bL = U * (((A + 2) * t + 2.25 * wd) / (1 + t) + 4 * L)
+    bH = (bL + U * ((A + 6) * wd + 2.25 * wdd + wd * ((A + 2) * t + 2.25 * wd) / (1 + t)) / (1 + t)
+          + 2 * U * (L + wd / (1 + t)))
     return bL, bH
 
 
