@@ -407,6 +407,142 @@ __global__ __launch_bounds__(64) void k_scores_join(const T* __restrict__ z, int
   }
 }
 
+// ------------------------------------------------------------- short rows
+// One thread per row of at most NC classes, the row in its registers.  A
+// wavefront reads 64 consecutive rows with 16-byte loads at each row's own
+// alignment (the hardware takes any), a row's loads back to back so that the
+// lines its lanes share are still in the L1.  The KT best are kept sorted by
+// insertion, a strict comparison from the lowest class up (so ties stay in
+// order); the first of them is the row's largest, left out of t.
+// Values [AT, AT + N) of the row, N values of at most 16 bytes; -inf past the end.
+template <typename T, int AT, int N, int NC>
+__device__ __forceinline__ void load_span(const T* __restrict__ row, int classes, float (&x)[NC]) {
+  if (AT + N <= classes) {
+    if constexpr (N == 1) {
+      x[AT] = ld(row + AT);
+    } else {
+      uint32_t w[N * sizeof(T) / 4];
+      __builtin_memcpy(w, row + AT, N * sizeof(T));
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        x[AT + i] = sizeof(T) == 4 ? __uint_as_float(w[i])
+                    : i % 2        ? __uint_as_float(w[i / 2] & 0xffff0000u)
+                                   : __uint_as_float(w[i / 2] << 16);
+    }
+  } else if constexpr (N > 1) {
+    load_span<T, AT, N / 2>(row, classes, x);
+    load_span<T, AT + N / 2, N / 2>(row, classes, x);
+  } else {
+    x[AT] = -INFINITY;
+  }
+}
+template <typename T, int NC, int AT = 0>
+__device__ __forceinline__ void load_row(const T* __restrict__ row, int classes, float (&x)[NC]) {
+  constexpr int V = 16 / (int)sizeof(T);
+  if constexpr (AT < NC) {
+    load_span<T, AT, V>(row, classes, x);
+    load_row<T, NC, AT + V>(row, classes, x);
+  }
+}
+
+template <typename T, int NC, int KT>
+__global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
+                                                    const int32_t* __restrict__ labels, int top_k, Outputs o) {
+  const int64_t r = (int64_t)blockIdx.x * 64 + threadIdx.x;
+  if (r >= n) return;
+  const T* row = z + r * ldz;
+  float x[NC];
+  load_row<T, NC>(row, classes, x);
+  const int lab = o.logprob ? labels[r] : -1;
+  float m = -INFINITY, tv[KT];
+  int ti[KT];
+#pragma unroll
+  for (int j = 0; j < KT; ++j) {
+    tv[j] = -INFINITY;
+    ti[j] = -1;
+  }
+#pragma unroll
+  for (int k0 = 0; k0 < NC; k0 += 4)
+    if (k0 < classes) {
+#pragma unroll
+      for (int k = k0; k < k0 + 4; ++k) {
+        const float v = x[k];  // -inf past the end: above nothing
+        m = OpMax::of(m, v);
+        bool above[KT];
+#pragma unroll
+        for (int j = 0; j < KT; ++j) above[j] = v > tv[j];
+#pragma unroll
+        for (int j = KT - 1; j >= 0; --j) {
+          const int up = j > 0 ? j - 1 : 0;
+          const bool shift = j > 0 && above[up];
+          tv[j] = shift ? tv[up] : above[j] ? v : tv[j];
+          ti[j] = shift ? ti[up] : above[j] ? k : ti[j];
+        }
+      }
+    }
+  Part p{m, 0.f, 0.f};
+  const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+  for (int k0 = 0; k0 < NC; k0 += 4)
+    if (k0 < classes) {
+#pragma unroll
+      for (int k = k0; k < k0 + 4; ++k) {
+        // 2^h, as in k_scores_chunk
+        const float h = fmaxf(k == ti[0] ? -INFINITY : (x[k] - base) * 1.44269504088896340736f, -300.f);
+        const float e = __builtin_amdgcn_exp2f(h);
+        p.t += e;
+        p.a = fmaf(e, h, p.a);
+      }
+    }
+  p.a *= 0.69314718055994530942f;
+  const float2 lh = finish(p);
+  if (o.logprob) o.logprob[r] = lab < 0 ? 0.f : lab >= classes ? NAN : (ld(row + lab) - base) - lh.x;
+  o.entropy[r] = lh.y;
+  reinterpret_cast<float2*>(o.stats)[r] = make_float2(m, lh.x);
+  if (top_k == 0) return;
+  if (m != m) {  // a NaN, which the comparisons passed over: one more pass per class
+    uint64_t last = ~0ull;
+    for (int j = 0; j < top_k; ++j) {
+      uint64_t best = 0;
+      for (int k = 0; k < classes; ++k) {
+        const uint64_t key = rank_key(ld(row + k), (uint32_t)k);
+        if (key < last && key > best) best = key;
+      }
+      last = best;
+      o.top_index[r * top_k + j] = (int32_t)key_class(best);
+      o.top_logprob[r * top_k + j] = NAN;
+    }
+    return;
+  }
+  int fill = 0;  // fewer classes above -inf than asked for: the lowest of the others follow
+#pragma unroll
+  for (int j = 0; j < KT; ++j)
+    if (j < top_k && tv[j] == -INFINITY) {
+      for (bool listed = true; listed;) {
+        listed = false;
+#pragma unroll
+        for (int i = 0; i < KT; ++i) listed |= tv[i] > -INFINITY && ti[i] == fill;
+        fill += listed;
+      }
+      ti[j] = fill++;
+    }
+  int32_t* ix = o.top_index + r * top_k;
+  float* lp = o.top_logprob + r * top_k;
+  if (top_k == KT) {  // one wide store
+#pragma unroll
+    for (int j = 0; j < KT; ++j) ix[j] = ti[j];
+#pragma unroll
+    for (int j = 0; j < KT; ++j) lp[j] = (tv[j] - base) - lh.x;
+  } else {
+#pragma unroll
+    for (int j = 0; j < KT; ++j)
+      if (j < top_k) {
+        ix[j] = ti[j];
+        lp[j] = (tv[j] - base) - lh.x;
+      }
+  }
+}
+
 // Which kernel takes a row, by its length alone (and, for rows of several
 // chunks, by how many there are): one workgroup holds up to 64 W E values.
 struct Route {
@@ -425,9 +561,35 @@ Route route_of(int64_t n, int classes) {
   return n * big >= 512 ? Route{4, 32, (int)big} : Route{4, 8, (int)ceil_div(len, 2048)};
 }
 
+constexpr int kRowMax = 64;  // classes of a row that one thread takes
+
+template <typename T, int NC>
+void launch_rows(const T* z, int64_t ldz, int64_t n, int classes, const int32_t* labels, int top_k, const Outputs& o,
+                 hipStream_t s) {
+  const unsigned g = (unsigned)ceil_div(n, 64);
+  if (top_k <= 1)
+    k_scores_rows<T, NC, 1><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o);
+  else if (top_k <= 3)
+    k_scores_rows<T, NC, 3><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o);
+  else if (top_k <= 8)
+    k_scores_rows<T, NC, 8><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o);
+  else
+    k_scores_rows<T, NC, 16><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o);
+}
+
 template <typename T>
-sscn_status launch_chunks(const T* z, int64_t ldz, int64_t n, int classes, const int32_t* labels, int top_k,
+sscn_status launch_scores(const T* z, int64_t ldz, int64_t n, int classes, const int32_t* labels, int top_k,
                           const Outputs& o, void* workspace, hipStream_t s) {
+  if (classes <= kRowMax) {
+    if (classes <= 16)
+      launch_rows<T, 16>(z, ldz, n, classes, labels, top_k, o, s);
+    else if (classes <= 32)
+      launch_rows<T, 32>(z, ldz, n, classes, labels, top_k, o, s);
+    else
+      launch_rows<T, 64>(z, ldz, n, classes, labels, top_k, o, s);
+    SSCN_HIP(hipGetLastError());
+    return SSCN_OK;
+  }
   const Route w = route_of(n, classes);
   const int64_t items = n * w.parts;
   float4* parts = (float4*)workspace;
@@ -497,8 +659,8 @@ extern "C" sscn_status sscn_label_scores(const void* logits, int64_t ldz, int64_
   if (n == 0) return SSCN_OK;
   const Outputs o{logprob, entropy, stats, top_index, top_logprob};
   return dtype == SSCN_F32
-             ? launch_chunks((const float*)logits, ldz, n, classes, labels, top_k, o, workspace, stream)
-             : launch_chunks((const uint16_t*)logits, ldz, n, classes, labels, top_k, o, workspace, stream);
+             ? launch_scores((const float*)logits, ldz, n, classes, labels, top_k, o, workspace, stream)
+             : launch_scores((const uint16_t*)logits, ldz, n, classes, labels, top_k, o, workspace, stream);
 }
 
 extern "C" sscn_status sscn_label_scores_backward(const void* logits, int64_t ldz, int64_t n, int32_t classes,
