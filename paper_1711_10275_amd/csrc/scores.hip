@@ -35,44 +35,6 @@ struct RowSums {
   float s, a;
   int eq;
 };
-// The gradient.  With A_k what class k receives directly (g = dlogprob where k
-// is the label, dtop_j where k is the j-th best class) and G their sum,
-//   dx_k = -A_k expm1(log p_k) - p_k ((G - A_k) + h (log p_k + H)),  h = dentropy,
-// which is A_k - p_k (G + h (log p_k + H)) without that form's cancellation
-// where p_k is close to 1.  One wavefront per row.
-template <typename T>
-__global__ __launch_bounds__(256) void k_scores_grad(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
-                                                     const int32_t* __restrict__ labels,
-                                                     const float* __restrict__ stats,
-                                                     const float* __restrict__ entropy, int top_k,
-                                                     const int32_t* __restrict__ top_index,
-                                                     const float* __restrict__ dlogprob,
-                                                     const float* __restrict__ dentropy,
-                                                     const float* __restrict__ dtop, T* __restrict__ dz,
-                                                     int64_t ldd) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int64_t r = (int64_t)blockIdx.x * 4 + wave; r < n; r += (int64_t)gridDim.x * 4) {
-    const T* row = z + r * ldz;
-    const float m = stats[2 * r], L = stats[2 * r + 1];
-    const bool empty = m == -INFINITY && L == 0.f;
-    const float h = dentropy ? dentropy[r] : 0.f, H = dentropy ? entropy[r] : 0.f;
-    const int lab = dlogprob ? labels[r] : -1;
-    const float g = lab < 0 ? 0.f : lab >= classes ? NAN : dlogprob[r];
-    float G = g;
-    if (dtop)
-      for (int j = 0; j < top_k; ++j) G += dtop[r * top_k + j];
-    for (int k = lane; k < classes; k += 64) {
-      float A = k == lab ? g : 0.f;
-      if (dtop)
-        for (int j = 0; j < top_k; ++j) A += top_index[r * top_k + j] == k ? dtop[r * top_k + j] : 0.f;
-      const float lp = (ld(row + k) - m) - L;
-      const float p = expf(lp);
-      const float v = -A * expm1f(lp) - p * ((G - A) + (p == 0.f ? 0.f : h * (lp + H)));
-      st(dz + r * ldd + k, empty ? 0.f : v);
-    }
-  }
-}
-
 // ------------------------------------------------------------- longer rows
 // A row is read as 16-byte (W = 1: 4-byte) pieces at their own alignment, so
 // that rows that start anywhere are read wide; the pieces at its ends that it
@@ -610,6 +572,188 @@ sscn_status launch_scores(const T* z, int64_t ldz, int64_t n, int classes, const
   return SSCN_OK;
 }
 
+// ------------------------------------------------------------- the gradient
+// With A_k what class k receives directly (g = dlogprob where k is the label,
+// dtop_j where k is the j-th best class), G their sum and h = dentropy,
+//   dx_k = -A_k expm1(log p_k) - p_k ((G - A_k) + h (log p_k + H)),
+// which is A_k - p_k (G + h (log p_k + H)) without that form's cancellation
+// where p_k is close to 1.  All but the label and the best classes have A_k = 0:
+// they are written as -p_k (G + h (log p_k + H)), and then those few again.
+struct GradInputs {
+  const int32_t* labels;
+  const float *stats, *entropy;
+  int top_k;                // 0 unless dtop is given
+  const int32_t* top_index;
+  const float *dlogprob, *dentropy, *dtop;
+};
+struct GradRow {
+  float base, L, h, H, g, G;
+  int lab;
+  bool empty;
+};
+__device__ __forceinline__ GradRow grad_row(const GradInputs& q, int64_t r, int classes) {
+  GradRow w;
+  const float2 st = reinterpret_cast<const float2*>(q.stats)[r];
+  w.L = st.y;
+  w.empty = st.x == -INFINITY && st.y == 0.f;
+  w.base = w.empty ? 0.f : st.x;
+  w.h = q.dentropy ? q.dentropy[r] : 0.f;
+  w.H = q.dentropy ? q.entropy[r] : 0.f;
+  w.lab = q.dlogprob ? q.labels[r] : -1;
+  w.g = w.lab < 0 ? 0.f : w.lab >= classes ? NAN : q.dlogprob[r];
+  w.G = w.g;
+  for (int j = 0; j < q.top_k; ++j) w.G += q.dtop[r * q.top_k + j];
+  if (w.L != w.L) w.G = NAN;  // the clamp below would lose it
+  if (w.empty) w.g = w.G = w.h = 0.f;
+  return w;
+}
+__device__ __forceinline__ float grad_dense(const GradRow& w, float x) {
+  const float lp = fmaxf((x - w.base) - w.L, -300.f);  // e^-300 is 0: no 0 * inf
+  return -__builtin_amdgcn_exp2f(lp * 1.44269504088896340736f) * fmaf(w.h, lp + w.H, w.G);
+}
+__device__ __forceinline__ float grad_direct(const GradRow& w, float x, float A) {
+  const float lp = (x - w.base) - w.L, p = expf(lp);
+  return -A * expm1f(lp) - p * ((w.G - A) + (p == 0.f ? 0.f : w.h * (lp + w.H)));
+}
+// What class k receives directly.
+__device__ __forceinline__ float direct_of(const GradInputs& q, const GradRow& w, int64_t r, int k) {
+  float A = k == w.lab ? w.g : 0.f;
+  for (int j = 0; j < q.top_k; ++j) A += q.top_index[r * q.top_k + j] == k ? q.dtop[r * q.top_k + j] : 0.f;
+  return w.empty ? 0.f : A;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {  // nearest even, NaN kept
+  typedef __bf16 B2 __attribute__((ext_vector_type(2)));
+  typedef float F2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(F2{lo, hi}, B2));
+}
+
+// Short rows, a thread per row as in k_scores_rows.  The 64 rows of a
+// wavefront go out through LDS, rows an odd number of words apart (each lane
+// its own bank), as consecutive words of 4 bytes (WORDS) or single values.
+template <typename T, int NC, bool WORDS>
+__global__ __launch_bounds__(64) void k_grad_rows(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
+                                                  GradInputs q, T* __restrict__ dz, int64_t ldd, int stride,
+                                                  uint32_t magic) {
+  extern __shared__ uint32_t lds[];
+  const int64_t r0 = (int64_t)blockIdx.x * 64, r = r0 + threadIdx.x;
+  T* out = reinterpret_cast<T*>(lds + threadIdx.x * stride);
+  if (r < n) {
+    const T* row = z + r * ldz;
+    float x[NC];
+    load_row<T, NC>(row, classes, x);
+    const GradRow w = grad_row(q, r, classes);
+#pragma unroll
+    for (int k0 = 0; k0 < NC; k0 += 4)
+      if (k0 < classes) {
+#pragma unroll
+        for (int k = k0; k < k0 + 4; ++k) x[k] = grad_dense(w, x[k]);
+        // whole words: the stride has room for a last group's unused values
+        if constexpr (sizeof(T) == 4) {
+          __builtin_memcpy(out + k0, x + k0, 16);
+        } else {
+          const uint32_t v[2] = {pack_bf16(x[k0], x[k0 + 1]), pack_bf16(x[k0 + 2], x[k0 + 3])};
+          __builtin_memcpy(out + k0, v, 8);
+        }
+      }
+    if (w.lab >= 0 && w.lab < classes) st(out + w.lab, grad_direct(w, ld(row + w.lab), direct_of(q, w, r, w.lab)));
+    for (int j = 0; j < q.top_k; ++j) {
+      const int k = q.top_index[r * q.top_k + j];
+      if (k >= 0 && k < classes) st(out + k, grad_direct(w, ld(row + k), direct_of(q, w, r, k)));
+    }
+  }
+  __syncthreads();
+  const int rows = (int)min<int64_t>(64, n - r0);
+  const int per = WORDS ? classes * (int)sizeof(T) / 4 : classes;  // items of a row
+  for (int i = threadIdx.x; i < rows * per; i += 64) {
+    const int row = (int)(((uint32_t)i * magic) >> 20), at = i - row * per;  // i / per, exact for i < 4096
+    T* to = dz + (r0 + row) * ldd;
+    if constexpr (WORDS)
+      reinterpret_cast<uint32_t*>(to)[at] = lds[row * stride + at];
+    else
+      to[at] = reinterpret_cast<const T*>(lds + row * stride)[at];
+  }
+}
+
+// Longer rows, a chunk of a row per turn of a workgroup.
+template <typename T, int W, int E>
+__global__ __launch_bounds__(64 * W) void k_grad_chunk(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
+                                                       int parts, GradInputs q, T* __restrict__ dz, int64_t ldd) {
+  using C = Chunk<T, W, E>;
+  const int64_t total = n * parts;
+  for (int64_t item = blockIdx.x; item < total; item += gridDim.x) {
+    const int64_t r = item / parts;
+    const T* row = z + r * ldz;
+    T* to = dz + r * ldd;
+    const int64_t c0 = (item - r * parts) * C::kPieces * C::V - C::head(row);
+    float x[C::G][C::V];
+    C::load(row, classes, c0, x);
+    const GradRow w = grad_row(q, r, classes);
+#pragma unroll
+    for (int g = 0; g < C::G; ++g) {
+#pragma unroll
+      for (int i = 0; i < C::V; ++i) x[g][i] = grad_dense(w, x[g][i]);
+      const int64_t k0 = c0 + ((int64_t)g * C::kThreads + threadIdx.x) * C::V;
+      if (k0 >= 0 && k0 + C::V <= classes) {  // one store, at whatever alignment it has
+        if constexpr (sizeof(T) == 4) {
+          __builtin_memcpy(to + k0, x[g], sizeof(T) * C::V);
+        } else {
+          uint32_t v[C::V / 2];
+#pragma unroll
+          for (int i = 0; i < C::V / 2; ++i) v[i] = pack_bf16(x[g][2 * i], x[g][2 * i + 1]);
+          __builtin_memcpy(to + k0, v, sizeof(T) * C::V);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < C::V; ++i)
+          if (k0 + i >= 0 && k0 + i < classes) st(to + k0 + i, x[g][i]);
+      }
+    }
+    __syncthreads();  // the chunk's stores come before those below
+    for (int j = threadIdx.x - 1; j < q.top_k; j += C::kThreads) {
+      const int k = j < 0 ? w.lab : q.top_index[r * q.top_k + j];
+      if (k >= 0 && k < classes && k >= c0 && k < c0 + C::kPieces * C::V)
+        st(to + k, grad_direct(w, ld(row + k), direct_of(q, w, r, k)));
+    }
+  }
+}
+
+template <typename T, int NC>
+void launch_grad_rows(const T* z, int64_t ldz, int64_t n, int classes, const GradInputs& q, T* dz, int64_t ldd,
+                      hipStream_t s) {
+  const int bytes = (int)sizeof(T) * classes;
+  const bool words = bytes % 4 == 0 && ldd * sizeof(T) % 4 == 0 && reinterpret_cast<uintptr_t>(dz) % 4 == 0;
+  const int stride = (int)(ceil_div(classes, 4) * 4 * sizeof(T) / 4) | 1;
+  const int per = words ? bytes / 4 : classes;
+  const uint32_t magic = ((1u << 20) + per - 1) / per;
+  const unsigned g = (unsigned)ceil_div(n, 64);
+  const size_t lds = (size_t)64 * stride * 4;
+  if (words)
+    k_grad_rows<T, NC, true><<<g, 64, lds, s>>>(z, ldz, n, classes, q, dz, ldd, stride, magic);
+  else
+    k_grad_rows<T, NC, false><<<g, 64, lds, s>>>(z, ldz, n, classes, q, dz, ldd, stride, magic);
+}
+
+template <typename T>
+sscn_status launch_grad(const T* z, int64_t ldz, int64_t n, int classes, const GradInputs& q, T* dz, int64_t ldd,
+                        hipStream_t s) {
+  if (classes <= 16) {
+    launch_grad_rows<T, 16>(z, ldz, n, classes, q, dz, ldd, s);
+  } else if (classes <= 32) {
+    launch_grad_rows<T, 32>(z, ldz, n, classes, q, dz, ldd, s);
+  } else if (classes <= kRowMax) {
+    launch_grad_rows<T, 64>(z, ldz, n, classes, q, dz, ldd, s);
+  } else if (classes <= 510) {
+    k_grad_chunk<T, 1, 8><<<(unsigned)std::min<int64_t>(n, 16384), 64, 0, s>>>(z, ldz, n, classes, 1, q, dz, ldd);
+  } else {
+    const int parts = (int)ceil_div((int64_t)classes + 7, 2048);
+    k_grad_chunk<T, 4, 8><<<(unsigned)std::min<int64_t>(n * parts, 16384), 256, 0, s>>>(z, ldz, n, classes, parts, q,
+                                                                                        dz, ldd);
+  }
+  SSCN_HIP(hipGetLastError());
+  return SSCN_OK;
+}
+
 sscn_status check_rows(const void* p, int64_t ld, int64_t n, int classes, sscn_dtype dtype) {
   if (dtype != SSCN_F32 && dtype != SSCN_BF16) return fail(SSCN_ERR_INVALID_ARG, "unknown dtype");
   if (n < 0 || classes < 1) return fail(SSCN_ERR_INVALID_ARG, "scores: n must be >= 0 and classes >= 1");
@@ -624,8 +768,6 @@ sscn_status check_top(int32_t top_k, int32_t classes) {
     return fail(SSCN_ERR_INVALID_ARG, "scores: top_k must be in [0, min(16, classes)]");
   return SSCN_OK;
 }
-
-unsigned wave_grid(int64_t n) { return (unsigned)std::min<int64_t>(ceil_div(n, 4), 1 << 20); }
 
 }  // namespace
 }  // namespace sscn
@@ -676,14 +818,7 @@ extern "C" sscn_status sscn_label_scores_backward(const void* logits, int64_t ld
   if (dlogprob && !labels) return fail(SSCN_ERR_INVALID_ARG, "scores: dlogprob without labels");
   if (dentropy && !entropy) return fail(SSCN_ERR_INVALID_ARG, "scores: dentropy without entropy");
   if (dtop && (top_k == 0 || !top_index)) return fail(SSCN_ERR_INVALID_ARG, "scores: dtop without top_index");
-  if (dtype == SSCN_F32)
-    k_scores_grad<float><<<wave_grid(n), 256, 0, stream>>>((const float*)logits, ldz, n, classes, labels, stats,
-                                                           entropy, top_k, top_index, dlogprob, dentropy, dtop,
-                                                           (float*)dlogits, ldd);
-  else
-    k_scores_grad<uint16_t><<<wave_grid(n), 256, 0, stream>>>((const uint16_t*)logits, ldz, n, classes, labels,
-                                                              stats, entropy, top_k, top_index, dlogprob, dentropy,
-                                                              dtop, (uint16_t*)dlogits, ldd);
-  SSCN_HIP(hipGetLastError());
-  return SSCN_OK;
+  const GradInputs q{labels, stats, entropy, dtop ? top_k : 0, top_index, dlogprob, dentropy, dtop};
+  return dtype == SSCN_F32 ? launch_grad((const float*)logits, ldz, n, classes, q, (float*)dlogits, ldd, stream)
+                           : launch_grad((const uint16_t*)logits, ldz, n, classes, q, (uint16_t*)dlogits, ldd, stream);
 }
