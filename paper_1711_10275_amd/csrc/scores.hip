@@ -29,12 +29,6 @@ __device__ __forceinline__ uint64_t rank_key(float x, uint32_t cls) {
 }
 __device__ __forceinline__ uint32_t key_class(uint64_t k) { return 0xffffffffu - (uint32_t)k; }
 
-// A row's sums: s over the values below m, eq = how many equal m, a = sum of
-// exp(d) d.
-struct RowSums {
-  float s, a;
-  int eq;
-};
 // ------------------------------------------------------------- longer rows
 // A row is read as 16-byte (W = 1: 4-byte) pieces at their own alignment, so
 // that rows that start anywhere are read wide; the pieces at its ends that it
@@ -47,6 +41,7 @@ struct Chunk {
   static constexpr int G = E / V;                               // pieces per thread
   static constexpr int kThreads = 64 * W;
   static constexpr int64_t kPieces = (int64_t)kThreads * G;     // per chunk
+  static constexpr int WORDS = V * (int)sizeof(T) / 4 > 0 ? V * (int)sizeof(T) / 4 : 1;
 
   // Class of value i of piece g of this thread, for the chunk that starts at class c0.
   __device__ static int cls(int64_t c0, int g, int i) {
@@ -55,41 +50,30 @@ struct Chunk {
   // Classes between the first whole piece's alignment and the row's start.
   __device__ static int head(const T* row) { return (int)(reinterpret_cast<uintptr_t>(row) % (V * sizeof(T)) / sizeof(T)); }
 
-  __device__ static void unpack(const T* piece, float (&x)[V]) {
-    if constexpr (V == 1) {
-      x[0] = ld(piece);
-    } else if constexpr (sizeof(T) == 4) {
-      const float4 q = *reinterpret_cast<const float4*>(piece);
-      x[0] = q.x; x[1] = q.y; x[2] = q.z; x[3] = q.w;
-    } else {
-      uint32_t w[V / 2];
-      if constexpr (V == 2) {
-        w[0] = *reinterpret_cast<const uint32_t*>(piece);
-      } else {
-        const uint4 q = *reinterpret_cast<const uint4*>(piece);
-        w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-      }
-#pragma unroll
-      for (int i = 0; i < V / 2; ++i) {
-        x[2 * i] = __uint_as_float(w[i] << 16);
-        x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      }
-    }
+  // The chunk as it is stored (bf16 two to a word), and its value i of piece g.
+  uint32_t w[G][WORDS];
+  __device__ float at(int g, int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[g][i]);
+    else return __uint_as_float(i % 2 ? w[g][i / 2] & 0xffff0000u : w[g][i / 2] << 16);
   }
-  // The chunk's values; -inf past the row's ends.  c0 = -head + chunk * kPieces * V.
-  __device__ static void load(const T* row, int classes, int64_t c0, float (&x)[G][V]) {
+  // -inf past the row's ends.  c0 = -head + chunk * kPieces * V.
+  __device__ void load(const T* row, int classes, int64_t c0) {
     const int64_t wave0 = c0 + (int64_t)(threadIdx.x & ~63) * V;  // first class of this wavefront's first piece
 #pragma unroll
     for (int g = 0; g < G; ++g) {
       const int64_t first = wave0 + (int64_t)g * kThreads * V;    // uniform in the wavefront
+      const int64_t k0 = first + (int64_t)(threadIdx.x & 63) * V;
       if (first >= 0 && first + 64 * V <= classes) {
-        unpack(row + (first + (int64_t)(threadIdx.x & 63) * V), x[g]);
+        __builtin_memcpy(w[g], __builtin_assume_aligned(row + k0, V * sizeof(T)), V * sizeof(T));
       } else {
+        const auto one = [&](int i) -> uint32_t {
+          const bool in = k0 + i >= 0 && k0 + i < classes;
+          if constexpr (sizeof(T) == 4) return in ? __float_as_uint(row[k0 + i]) : 0xff800000u;
+          else return in ? row[k0 + i] : 0xff80u;
+        };
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const int64_t k = first + (int64_t)(threadIdx.x & 63) * V + i;
-          x[g][i] = k >= 0 && k < classes ? ld(row + k) : -INFINITY;
-        }
+        for (int i = 0; i < WORDS; ++i)
+          w[g][i] = sizeof(T) == 4 ? one(i) : one(2 * i) | one(2 * i + 1) << 16;
       }
     }
   }
@@ -164,31 +148,31 @@ __device__ __forceinline__ void write_row(const T* row, int64_t r, int classes, 
 // threads that share no value), is no larger than the top_k-th best value, so
 // what is below T is out.  Few values are left (about top_k log(top_k) of
 // unordered ones); each counts the keys above its own, which is its rank.
-// Values of -inf stay out of the lists.  A list that overflows (ties at T), or
-// a NaN, takes the slow way: one more pass over the registers per class.
+// Values of -inf stay out of the list.  Masks that leave some group nothing
+// make T -inf: the largest is taken off a long list top_k times.  A list that
+// overflows (ties at T), or a NaN, takes them off the row itself.
 template <typename T, int W, int E>
 __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
-                                                         int parts, const int32_t* __restrict__ labels, int top_k,
-                                                         Outputs o, float4* __restrict__ part_out,
+                                                         const int32_t* __restrict__ labels, int top_k, Outputs o,
+                                                         float4* __restrict__ part_out,
                                                          uint64_t* __restrict__ keys_out) {
   using C = Chunk<T, W, E>;
-  constexpr int kList = 64 * W * E < 2048 ? 64 * W * E : 2048;
-  __shared__ uint64_t list[kList], top[kMaxTop];
-  __shared__ float red[3][W];
-  __shared__ int count, ties[W];
+  constexpr int kList = 64 * W * E < 2048 ? 64 * W * E : 2048, kRanked = 128;
+  __shared__ uint64_t list[kList], top[kMaxTop], most[2][W];
+  __shared__ float red[2][W], sums[3][W];
+  __shared__ int count;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t total = n * parts;
-  for (int64_t item = blockIdx.x; item < total; item += gridDim.x) {
-    const int64_t r = item / parts;
+  const int parts = (int)gridDim.x;
+  for (int64_t r = blockIdx.y; r < n; r += gridDim.y) {
     const T* row = z + r * ldz;
-    const int64_t c0 = (item - r * parts) * C::kPieces * C::V - C::head(row);
-    float x[C::G][C::V];
-    C::load(row, classes, c0, x);
+    const int64_t c0 = (int64_t)blockIdx.x * (C::kPieces * C::V) - C::head(row);
+    C x;
+    x.load(row, classes, c0);
     float own = -INFINITY;  // this thread's maximum
 #pragma unroll
     for (int g = 0; g < C::G; ++g)
 #pragma unroll
-      for (int i = 0; i < C::V; ++i) own = OpMax::of(own, x[g][i]);
+      for (int i = 0; i < C::V; ++i) own = OpMax::of(own, x.at(g, i));
     // maxima of groups of lanes, and the threshold from them
     const float v4 = wave_reduce<OpMax, 1, 4>(own), v8 = wave_reduce<OpMax, 4, 8>(v4);
     const float v16 = wave_reduce<OpMax, 8, 16>(v8), v32 = wave_reduce<OpMax, 16, 32>(v16);
@@ -213,8 +197,7 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
       m = OpMax::of(OpMax::of(m0, m1), OpMax::of(m2, m3));
       const float least = fminf(fminf(red[1][0], red[1][1]), fminf(red[1][2], red[1][3]));
       // of four maxima the first, second, third or fourth largest
-      const float hi0 = fmaxf(m0, m1), lo0 = fminf(m0, m1), hi1 = fmaxf(m2, m3), lo1 = fminf(m2, m3);
-      const float mid0 = fminf(hi0, hi1), mid1 = fmaxf(lo0, lo1);
+      const float mid0 = fminf(fmaxf(m0, m1), fmaxf(m2, m3)), mid1 = fmaxf(fminf(m0, m1), fminf(m2, m3));
       cut = top_k == 1 ? m : top_k == 2 ? fmaxf(mid0, mid1) : top_k == 3 ? fminf(mid0, mid1) : least;
     }
     if (top_k > 0 && m == m) {
@@ -222,75 +205,77 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
       for (int g = 0; g < C::G; ++g)
 #pragma unroll
         for (int i = 0; i < C::V; ++i)
-          if (x[g][i] >= cut && x[g][i] > -INFINITY) {
+          if (x.at(g, i) >= cut && x.at(g, i) > -INFINITY) {
             const int at = atomicAdd(&count, 1);
-            if (at < kList) list[at] = rank_key(x[g][i], (uint32_t)C::cls(c0, g, i));
+            if (at < kList) list[at] = rank_key(x.at(g, i), (uint32_t)C::cls(c0, g, i));
           }
     }
-    // the sums, of 2^h with h = (x - m) log2(e): the largest are counted and
-    // left out.  h is one rounded product: a term is off by up to 2.25 |x - m|
-    // half steps, which its own size e^(x - m) outweighs; forming the product's
-    // low part too would cost three more operations a value.
-    RowSums q{0.f, 0.f, 0};
-    float y[C::G][C::V];
-#pragma unroll
-    for (int g = 0; g < C::G; ++g)
-#pragma unroll
-      for (int i = 0; i < C::V; ++i) y[g][i] = x[g][i];
-    if (own == m) {
+    // The sums, of 2^h with h = (x - m) log2(e): the largest are counted and
+    // left out (only a wavefront that holds one looks for them).  h is one
+    // rounded product: a term is off by up to 2.25 |x - m| half steps, which its
+    // own size e^(x - m) outweighs; forming the product's low part too would
+    // cost three more operations a value.
+    float s = 0.f, a = 0.f, eq = 0.f;
+    const float base = m == -INFINITY ? 0.f : m;
+    const auto add = [&](float v) {
+      const float h = fmaxf((v - base) * 1.44269504088896340736f, -300.f);  // 2^-300 is 0
+      const float e = __builtin_amdgcn_exp2f(h);
+      s += e;
+      a = fmaf(e, h, a);
+    };
+    if (__ballot(own == m) != 0) {
 #pragma unroll
       for (int g = 0; g < C::G; ++g)
 #pragma unroll
-        for (int i = 0; i < C::V; ++i)
-          if (y[g][i] == m) {
-            y[g][i] = -INFINITY;
-            ++q.eq;
-          }
+        for (int i = 0; i < C::V; ++i) {
+          const bool largest = x.at(g, i) == m;
+          eq += largest ? 1.f : 0.f;
+          add(largest ? -INFINITY : x.at(g, i));
+        }
+      eq = wave_reduce<OpAdd>(eq);  // at most 8192: exact
+    } else {
+#pragma unroll
+      for (int g = 0; g < C::G; ++g)
+#pragma unroll
+        for (int i = 0; i < C::V; ++i) add(x.at(g, i));
     }
-    const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int g = 0; g < C::G; ++g)
-#pragma unroll
-      for (int i = 0; i < C::V; ++i) {
-        const float h = fmaxf((y[g][i] - base) * 1.44269504088896340736f, -300.f);  // 2^-300 is 0
-        const float e = __builtin_amdgcn_exp2f(h);
-        q.s += e;
-        q.a = fmaf(e, h, q.a);
-      }
-    q.s = wave_reduce<OpAdd>(q.s);
-    q.a = wave_reduce<OpAdd>(q.a) * 0.69314718055994530942f;
-    q.eq = (int)wave_reduce<OpAdd>((float)q.eq);  // at most 8192: exact
+    s = wave_reduce<OpAdd>(s);
+    a = wave_reduce<OpAdd>(a) * 0.69314718055994530942f;
     if constexpr (W > 1) {
       if (lane == 0) {
-        red[2][wave] = q.s;
-        ties[wave] = q.eq;
+        sums[0][wave] = s;
+        sums[1][wave] = a;
+        sums[2][wave] = eq;
       }
-      __syncthreads();  // also: every wavefront has read red[0] and red[1]
-      if (lane == 0) red[1][wave] = q.a;
-      q.s = (red[2][0] + red[2][1]) + (red[2][2] + red[2][3]);
-      q.eq = (ties[0] + ties[1]) + (ties[2] + ties[3]);
     }
     __syncthreads();
-    if constexpr (W > 1) q.a = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
     const int found = count;
     if (top_k > 0) {
-      if (m != m || found > kList) {
+      if (m != m || found > kRanked) {
+        const bool listed = m == m && found <= kList;
         uint64_t last = ~0ull;
         for (int j = 0; j < top_k; ++j) {
           uint64_t best = 0;
-#pragma unroll
-          for (int g = 0; g < C::G; ++g)
-#pragma unroll
-            for (int i = 0; i < C::V; ++i) {
-              const uint64_t key = rank_key(x[g][i], (uint32_t)C::cls(c0, g, i));
-              if (!(x[g][i] == -INFINITY) && key < last && key > best) best = key;
+          if (listed) {
+#pragma nounroll
+            for (int i = threadIdx.x; i < found; i += C::kThreads) {
+              const uint64_t key = list[i];
+              if (key < last && key > best) best = key;
             }
+          } else {
+            const int first = (int)max<int64_t>(c0, 0), end = (int)min<int64_t>(c0 + C::kPieces * C::V, classes);
+#pragma nounroll
+            for (int k = first + threadIdx.x; k < end; k += C::kThreads) {
+              const float v = ld(row + k);
+              const uint64_t key = rank_key(v, (uint32_t)k);
+              if (!(v == -INFINITY) && key < last && key > best) best = key;
+            }
+          }
           best = wave_max_key(best);
           if constexpr (W > 1) {
+            if (lane == 0) most[j & 1][wave] = best;
             __syncthreads();
-            if (lane == 0) list[wave] = best;
-            __syncthreads();
-            best = max(max(list[0], list[1]), max(list[2], list[3]));
+            best = max(max(most[j & 1][0], most[j & 1][1]), max(most[j & 1][2], most[j & 1][3]));
           }
           last = best;
           if (threadIdx.x == 0) top[j] = best;
@@ -305,11 +290,17 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
       }
       __syncthreads();
     }
-    const Part p{m, m == -INFINITY ? 0.f : q.s + (float)(q.eq - 1), q.a};
     if (wave == 0) {
+      if constexpr (W > 1) {
+        s = (sums[0][0] + sums[0][1]) + (sums[0][2] + sums[0][3]);
+        a = (sums[1][0] + sums[1][1]) + (sums[1][2] + sums[1][3]);
+        eq = (sums[2][0] + sums[2][1]) + (sums[2][2] + sums[2][3]);
+      }
+      const Part p{m, m == -INFINITY ? 0.f : s + (eq - 1.f), a};
       if (parts == 1) {
         write_row(row, r, classes, labels, top_k, p, top, o);
       } else {
+        const int64_t item = r * parts + blockIdx.x;
         if (lane == 0) part_out[item] = make_float4(p.m, p.t, p.a, 0.f);
         if (lane < top_k) keys_out[item * top_k + lane] = top[lane];
       }
@@ -556,13 +547,14 @@ sscn_status launch_scores(const T* z, int64_t ldz, int64_t n, int classes, const
   const int64_t items = n * w.parts;
   float4* parts = (float4*)workspace;
   uint64_t* keys = (uint64_t*)(parts + items);
-  const unsigned g = (unsigned)std::min<int64_t>(items, w.waves == 1 ? 16384 : 8192);
+  // a workgroup takes rows in turn once there are some 16384 of them
+  const dim3 g((unsigned)w.parts, (unsigned)std::max<int64_t>(1, std::min<int64_t>(n, 16384 / w.parts)));
   if (w.waves == 1)
-    k_scores_chunk<T, 1, 8><<<g, 64, 0, s>>>(z, ldz, n, classes, w.parts, labels, top_k, o, parts, keys);
+    k_scores_chunk<T, 1, 8><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
   else if (w.per_thread == 8)
-    k_scores_chunk<T, 4, 8><<<g, 256, 0, s>>>(z, ldz, n, classes, w.parts, labels, top_k, o, parts, keys);
+    k_scores_chunk<T, 4, 8><<<g, 256, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
   else
-    k_scores_chunk<T, 4, 32><<<g, 256, 0, s>>>(z, ldz, n, classes, w.parts, labels, top_k, o, parts, keys);
+    k_scores_chunk<T, 4, 32><<<g, 256, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
   SSCN_HIP(hipGetLastError());
   if (w.parts > 1) {
     k_scores_join<T><<<(unsigned)std::min<int64_t>(n, 16384), 64, 0, s>>>(z, ldz, n, classes, w.parts, labels, top_k, o,
@@ -686,27 +678,28 @@ __global__ __launch_bounds__(64 * W) void k_grad_chunk(const T* __restrict__ z, 
     const T* row = z + r * ldz;
     T* to = dz + r * ldd;
     const int64_t c0 = (item - r * parts) * C::kPieces * C::V - C::head(row);
-    float x[C::G][C::V];
-    C::load(row, classes, c0, x);
+    C chunk;
+    chunk.load(row, classes, c0);
     const GradRow w = grad_row(q, r, classes);
 #pragma unroll
     for (int g = 0; g < C::G; ++g) {
+      float x[C::V];
 #pragma unroll
-      for (int i = 0; i < C::V; ++i) x[g][i] = grad_dense(w, x[g][i]);
+      for (int i = 0; i < C::V; ++i) x[i] = grad_dense(w, chunk.at(g, i));
       const int64_t k0 = c0 + ((int64_t)g * C::kThreads + threadIdx.x) * C::V;
       if (k0 >= 0 && k0 + C::V <= classes) {  // one store, at whatever alignment it has
         if constexpr (sizeof(T) == 4) {
-          __builtin_memcpy(to + k0, x[g], sizeof(T) * C::V);
+          __builtin_memcpy(to + k0, x, sizeof(T) * C::V);
         } else {
           uint32_t v[C::V / 2];
 #pragma unroll
-          for (int i = 0; i < C::V / 2; ++i) v[i] = pack_bf16(x[g][2 * i], x[g][2 * i + 1]);
+          for (int i = 0; i < C::V / 2; ++i) v[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
           __builtin_memcpy(to + k0, v, sizeof(T) * C::V);
         }
       } else {
 #pragma unroll
         for (int i = 0; i < C::V; ++i)
-          if (k0 + i >= 0 && k0 + i < classes) st(to + k0 + i, x[g][i]);
+          if (k0 + i >= 0 && k0 + i < classes) st(to + k0 + i, x[i]);
       }
     }
     __syncthreads();  // the chunk's stores come before those below
