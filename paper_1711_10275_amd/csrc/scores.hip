@@ -9,6 +9,7 @@
 // log probability is -t, where log(1 + t) would have dropped t's low bits.
 // Sums are fp32, over the values as they are stored.
 #include <algorithm>
+#include <type_traits>
 
 #include "internal.h"
 #include "numeric.h"
@@ -28,54 +29,59 @@ __device__ __forceinline__ uint64_t rank_key(float x, uint32_t cls) {
   return (uint64_t)o << 32 | (0xffffffffu - cls);
 }
 __device__ __forceinline__ uint32_t key_class(uint64_t k) { return 0xffffffffu - (uint32_t)k; }
+__device__ __forceinline__ float key_value(uint64_t k) {  // NaN for NaN, 0 for -0
+  const uint32_t o = (uint32_t)(k >> 32);
+  return __uint_as_float((int32_t)o < 0 ? o & 0x7fffffffu : ~o);
+}
 
 // ------------------------------------------------------------- longer rows
-// A row is read as 16-byte (W = 1: 4-byte) pieces at their own alignment, so
-// that rows that start anywhere are read wide; the pieces at its ends that it
-// shares with its neighbours are read value by value. A workgroup of W
-// wavefronts holds a chunk of 64 W E values in registers, E a thread: one read
-// of the logits, the maximum before the exponentials.
-template <typename T, int W, int E>
+// A team of L lanes (L = 16 or 64: within one wavefront; L = 256: a workgroup)
+// holds a chunk of up to L E values of a row in registers as they are stored:
+// one read of the logits, the maximum before the exponentials.  Lanes take
+// 16-byte pieces of V values, from the row's start on and at whatever alignment
+// that has (the hardware takes any).  A piece that the row's end cuts is the
+// row's last V values, of which those of the piece before are made -inf; so is
+// all of a piece beyond the end.
+template <typename T, int L, int E>
 struct Chunk {
-  static constexpr int V = (W == 1 ? 4 : 16) / (int)sizeof(T);  // values per piece
-  static constexpr int G = E / V;                               // pieces per thread
-  static constexpr int kThreads = 64 * W;
-  static constexpr int64_t kPieces = (int64_t)kThreads * G;     // per chunk
-  static constexpr int WORDS = V * (int)sizeof(T) / 4 > 0 ? V * (int)sizeof(T) / 4 : 1;
+  static constexpr int V = 16 / (int)sizeof(T);  // values per piece
+  static constexpr int G = E / V;                // pieces per lane
+  static constexpr int kSpan = L * V;            // values of the team's g-th pieces
+  static constexpr int kValues = L * E;
 
-  // Class of value i of piece g of this thread, for the chunk that starts at class c0.
-  __device__ static int cls(int64_t c0, int g, int i) {
-    return (int)(c0 + ((int64_t)g * kThreads + threadIdx.x) * V + i);
-  }
-  // Classes between the first whole piece's alignment and the row's start.
-  __device__ static int head(const T* row) { return (int)(reinterpret_cast<uintptr_t>(row) % (V * sizeof(T)) / sizeof(T)); }
+  uint32_t w[G][4];  // bf16 two to a word
+  int lane, len;     // lane of the team; values of the chunk, V <= len <= kValues
 
-  // The chunk as it is stored (bf16 two to a word), and its value i of piece g.
-  uint32_t w[G][WORDS];
+  // Whether the g-th pieces hold anything: the same for the whole team.
+  __device__ bool has(int g) const { return g * kSpan < len; }
+  // Place in the chunk of this lane's piece g.
+  __device__ int place(int g) const { return min((g * L + lane) * V, len - V); }
   __device__ float at(int g, int i) const {
     if constexpr (sizeof(T) == 4) return __uint_as_float(w[g][i]);
     else return __uint_as_float(i % 2 ? w[g][i / 2] & 0xffff0000u : w[g][i / 2] << 16);
   }
-  // -inf past the row's ends.  c0 = -head + chunk * kPieces * V.
-  __device__ void load(const T* row, int classes, int64_t c0) {
-    const int64_t wave0 = c0 + (int64_t)(threadIdx.x & ~63) * V;  // first class of this wavefront's first piece
+  __device__ void load(const T* p, int lane_, int len_) {
+    lane = lane_;
+    len = len_;
+    // Each turn forms the places and masks below anew: kept over the row loop
+    // they took 70 more registers, and half of the wavefronts that fit.
+    asm volatile("" : "+v"(lane), "+s"(len));
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const int64_t first = wave0 + (int64_t)g * kThreads * V;    // uniform in the wavefront
-      const int64_t k0 = first + (int64_t)(threadIdx.x & 63) * V;
-      if (first >= 0 && first + 64 * V <= classes) {
-        __builtin_memcpy(w[g], __builtin_assume_aligned(row + k0, V * sizeof(T)), V * sizeof(T));
-      } else {
-        const auto one = [&](int i) -> uint32_t {
-          const bool in = k0 + i >= 0 && k0 + i < classes;
-          if constexpr (sizeof(T) == 4) return in ? __float_as_uint(row[k0 + i]) : 0xff800000u;
-          else return in ? row[k0 + i] : 0xff80u;
-        };
+    for (int g = 0; g < G; ++g)
+      if (has(g)) __builtin_memcpy(w[g], p + place(g), 16);
 #pragma unroll
-        for (int i = 0; i < WORDS; ++i)
-          w[g][i] = sizeof(T) == 4 ? one(i) : one(2 * i) | one(2 * i + 1) << 16;
+    for (int g = 0; g < G; ++g)
+      if (has(g) && (g + 1) * kSpan > len) {
+        const int twice = (g * L + lane) * V - place(g);  // values that the pieces before have
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if constexpr (sizeof(T) == 4) {
+            w[g][i] = i < twice ? 0xff800000u : w[g][i];  // -inf
+          } else {
+            const uint32_t none = i % 2 ? 0xff800000u : 0xff80u, rest = i % 2 ? 0xffffu : 0xffff0000u;
+            w[g][i / 2] = i < twice ? (w[g][i / 2] & rest) | none : w[g][i / 2];
+          }
       }
-    }
   }
 };
 
@@ -104,13 +110,22 @@ struct Outputs {
   int32_t* top_index;
   float* top_logprob;
 };
-
-// Writes row r.  top: top_k keys in LDS, best first, 0 where the row has fewer
-// classes above -inf: the lowest of the others follow.
+// A row's label and its logit, read before the row's work.
+struct Label {
+  int k;
+  float x;
+};
 template <typename T>
-__device__ __forceinline__ void write_row(const T* row, int64_t r, int classes, const int32_t* labels, int top_k,
-                                          const Part& p, uint64_t* top, const Outputs& o) {
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ Label label_of(const T* row, const int32_t* labels, int64_t r, int classes) {
+  const int k = labels ? labels[r] : -1;
+  return {k, k >= 0 && k < classes ? ld(row + k) : k < 0 ? 0.f : NAN};
+}
+
+// Writes row r, by lanes 0 .. 15 of a team.  top: top_k keys in LDS, best
+// first, 0 where the row has fewer classes above -inf: the lowest of the
+// others follow.
+__device__ __forceinline__ void write_row(int lane, int64_t r, const Label& lab, int top_k, const Part& p,
+                                          uint64_t* top, const Outputs& o) {
   const float2 lh = finish(p);
   const float base = p.m == -INFINITY ? 0.f : p.m;
   if (top_k > 0 && lane == 0 && top[top_k - 1] == 0) {
@@ -124,67 +139,97 @@ __device__ __forceinline__ void write_row(const T* row, int64_t r, int classes, 
     }
   }
   if (lane == 0) {
-    if (o.logprob) {
-      const int lab = labels[r];
-      o.logprob[r] = lab < 0 ? 0.f : lab >= classes ? NAN : (ld(row + lab) - base) - lh.x;
-    }
+    if (o.logprob) o.logprob[r] = lab.k < 0 ? 0.f : (lab.x - base) - lh.x;
     o.entropy[r] = lh.y;
-    o.stats[2 * r] = p.m;
-    o.stats[2 * r + 1] = lh.x;
+    reinterpret_cast<float2*>(o.stats)[r] = make_float2(p.m, lh.x);
   }
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   if (lane < top_k) {
-    const uint32_t k = key_class(top[lane]);
-    o.top_index[r * top_k + lane] = (int32_t)k;
-    o.top_logprob[r * top_k + lane] = (ld(row + k) - base) - lh.x;
+    const uint64_t key = top[lane];
+    o.top_index[r * top_k + lane] = (int32_t)key_class(key);
+    o.top_logprob[r * top_k + lane] = (key_value(key) - base) - lh.x;
   }
 }
 
-// One chunk of one row per turn of a workgroup; `parts` chunks per row.  With
-// one the row is written, with more its Part and its best keys are left for
-// k_scores_join.
+// Teams of W wavefronts (W = 1: 64 / L teams to a workgroup of one wavefront,
+// a whole row each; W = 4: L = 64 lanes of each wavefront together, one chunk
+// of one row, blockIdx.x the chunk).  Where a row is one chunk it is written,
+// else its Part and its best keys are left for k_scores_join.
 //
 // The best classes: T, the least of at least top_k groups' maxima (groups of
-// threads that share no value), is no larger than the top_k-th best value, so
+// lanes that share no value), is no larger than the top_k-th best value, so
 // what is below T is out.  Few values are left (about top_k log(top_k) of
 // unordered ones); each counts the keys above its own, which is its rank.
 // Values of -inf stay out of the list.  Masks that leave some group nothing
 // make T -inf: the largest is taken off a long list top_k times.  A list that
 // overflows (ties at T), or a NaN, takes them off the row itself.
-template <typename T, int W, int E>
+// KT: at most as many best classes (0, 8 or 16: what fewer need takes fewer
+// registers).
+template <typename T, int L, int W, int E, int KT>
 __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
                                                          const int32_t* __restrict__ labels, int top_k, Outputs o,
                                                          float4* __restrict__ part_out,
                                                          uint64_t* __restrict__ keys_out) {
-  using C = Chunk<T, W, E>;
-  constexpr int kList = 64 * W * E < 2048 ? 64 * W * E : 2048, kRanked = 128;
-  __shared__ uint64_t list[kList], top[kMaxTop], most[2][W];
+  using C = Chunk<T, L * W, E>;
+  constexpr int kTeams = 64 / L;  // to a wavefront
+  // keys that a wavefront's part of a team may list, and may rank
+  constexpr int kList = L == 16 ? 128 : L * E < 512 ? L * E : 512, kRanked = 128 / W;
+  __shared__ uint64_t lists[kTeams * W][kList], tops[kTeams][kMaxTop], most[2][W];
   __shared__ float red[2][W], sums[3][W];
-  __shared__ int count;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int parts = (int)gridDim.x;
-  for (int64_t r = blockIdx.y; r < n; r += gridDim.y) {
+  __shared__ int counts[W];
+  static_assert(W == 1 || (W == 4 && L == 64));
+  const int wave = threadIdx.x >> 6;
+  const int team = (threadIdx.x & 63) / L, lane = threadIdx.x & (L - 1);  // lane of the team's part of this wavefront
+  const int all = W == 1 ? lane : (int)threadIdx.x;                       // lane of the team
+  uint64_t *list = lists[W == 1 ? team : wave], *top = tops[team];
+  const int parts = W == 1 ? 1 : (int)gridDim.x;
+  const int64_t rows = W == 1 ? (int64_t)gridDim.x * kTeams : gridDim.y;
+  for (int64_t r0 = W == 1 ? (int64_t)blockIdx.x * kTeams : blockIdx.y; r0 < n; r0 += rows) {
+    const int64_t r = min<int64_t>(r0 + team, n - 1);
+    const bool live = r0 + team < n;  // a last team without a row works on the last one, and does not write
     const T* row = z + r * ldz;
-    const int64_t c0 = (int64_t)blockIdx.x * (C::kPieces * C::V) - C::head(row);
+    const int k0 = W == 1 ? 0 : (int)blockIdx.x * C::kValues;
     C x;
-    x.load(row, classes, c0);
-    float own = -INFINITY;  // this thread's maximum
+    x.load(row + k0, all, min(classes - k0, C::kValues));
+    Label lab{-1, 0.f};
+    if (wave == 0 && lane == 0) lab = label_of(row, labels, r, classes);
+    // this lane's maxima: of its pieces, of all their first and second halves
+    float piece[C::G], half0 = -INFINITY, half1 = -INFINITY;
 #pragma unroll
-    for (int g = 0; g < C::G; ++g)
+    for (int g = 0; g < C::G; ++g) {
+      piece[g] = -INFINITY;
+      if (!x.has(g)) continue;
+      float m0 = x.at(g, 0), m1 = x.at(g, C::V / 2);
 #pragma unroll
-      for (int i = 0; i < C::V; ++i) own = OpMax::of(own, x.at(g, i));
-    // maxima of groups of lanes, and the threshold from them
-    const float v4 = wave_reduce<OpMax, 1, 4>(own), v8 = wave_reduce<OpMax, 4, 8>(v4);
-    const float v16 = wave_reduce<OpMax, 8, 16>(v8), v32 = wave_reduce<OpMax, 16, 32>(v16);
-    float m = wave_reduce<OpMax, 32, 64>(v32), cut = m;
-    if constexpr (W == 1) {
-      if (top_k > 1) cut = wave_reduce<OpMin>(top_k <= 2 ? v32 : top_k <= 4 ? v16 : top_k <= 8 ? v8 : v4);
-    } else {
-      static_assert(W == 4);
-      if (top_k > 4) cut = wave_reduce<OpMin>(top_k <= 8 ? v32 : v16);
+      for (int i = 1; i < C::V / 2; ++i) {
+        m0 = OpMax::of(m0, x.at(g, i));
+        m1 = OpMax::of(m1, x.at(g, C::V / 2 + i));
+      }
+      piece[g] = OpMax::of(m0, m1);
+      half0 = OpMax::of(half0, m0);
+      half1 = OpMax::of(half1, m1);
     }
-    if (threadIdx.x == 0) count = 0;
-    if (threadIdx.x < kMaxTop) top[threadIdx.x] = 0;
+    const float own = OpMax::of(half0, half1);
+    // the threshold: of 16 lanes the top_k-th largest maximum (of 64 lanes, the
+    // least of the four rows' top_k / 4-th), or of the maxima of groups
+    float m = wave_reduce<OpMax, 1, L>(own), cut = m;
+    if constexpr (KT == 0) {
+    } else if constexpr (L == 16) {
+      if (KT > 8 && top_k > 8) {
+        const float lo = fminf(half0, half1);  // own and lo, of each lane
+        const int above_own = above_in_row(own, own) + above_in_row(lo, own);
+        const int above_lo = above_in_row(own, lo) + above_in_row(lo, lo) + (own > lo);
+        cut = wave_reduce<OpMin, 1, 16>(above_lo < top_k ? lo : above_own < top_k ? own : INFINITY);
+      } else if (top_k > 1) {
+        cut = wave_reduce<OpMin, 1, 16>(above_in_row(own, own) < top_k ? own : INFINITY);
+      }
+    } else if constexpr (W == 1) {
+      if (top_k > 1) cut = wave_reduce<OpMin>(above_in_row(own, own) < (top_k + 3) / 4 ? own : INFINITY);
+    } else if (top_k > 4) {
+      const float v16 = wave_reduce<OpMax, 1, 16>(own);
+      cut = wave_reduce<OpMin, 16, 64>(top_k <= 8 ? wave_reduce<OpMax, 16, 32>(v16) : v16);
+    }
+    if (all < kMaxTop) top[all] = 0;
     if constexpr (W > 1) {
       if (lane == 0) {
         red[0][wave] = m;
@@ -200,21 +245,33 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
       const float mid0 = fminf(fmaxf(m0, m1), fmaxf(m2, m3)), mid1 = fmaxf(fminf(m0, m1), fminf(m2, m3));
       cut = top_k == 1 ? m : top_k == 2 ? fmaxf(mid0, mid1) : top_k == 3 ? fminf(mid0, mid1) : least;
     }
-    if (top_k > 0 && m == m) {
+    int count = 0;  // keys listed by this wavefront's part of the team
+    cut = fmaxf(cut, -3.402823466e38f);  // -inf stays out
+    if (KT > 0 && top_k > 0) {
 #pragma unroll
-      for (int g = 0; g < C::G; ++g)
+      for (int g = 0; g < C::G; ++g) {
+        if (!x.has(g) || __ballot(piece[g] >= cut) == 0) continue;
 #pragma unroll
-        for (int i = 0; i < C::V; ++i)
-          if (x.at(g, i) >= cut && x.at(g, i) > -INFINITY) {
-            const int at = atomicAdd(&count, 1);
-            if (at < kList) list[at] = rank_key(x.at(g, i), (uint32_t)C::cls(c0, g, i));
+        for (int i = 0; i < C::V; ++i) {
+          const float v = x.at(g, i);
+          const bool in = v >= cut;
+          uint64_t mask = __ballot(in);
+          if (mask == 0) continue;
+          if constexpr (L < 64) mask = mask >> (team * L) & ((1ull << L) - 1);
+          if (in) {
+            const int at = count + (L < 64 ? __popc((uint32_t)mask & ((1u << lane) - 1))
+                                           : (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)));
+            if (at < kList) list[at] = rank_key(v, (uint32_t)(k0 + x.place(g) + i));
           }
+          count += __popcll(mask);
+        }
+      }
     }
     // The sums, of 2^h with h = (x - m) log2(e): the largest are counted and
-    // left out (only a wavefront that holds one looks for them).  h is one
-    // rounded product: a term is off by up to 2.25 |x - m| half steps, which its
-    // own size e^(x - m) outweighs; forming the product's low part too would
-    // cost three more operations a value.
+    // left out (only pieces that hold one are searched).  h is one rounded
+    // product: a term is off by up to 2.25 |x - m| half steps, which its own
+    // size e^(x - m) outweighs; forming the product's low part too would cost
+    // three more operations a value.
     float s = 0.f, a = 0.f, eq = 0.f;
     const float base = m == -INFINITY ? 0.f : m;
     const auto add = [&](float v) {
@@ -223,74 +280,79 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
       s += e;
       a = fmaf(e, h, a);
     };
-    if (__ballot(own == m) != 0) {
 #pragma unroll
-      for (int g = 0; g < C::G; ++g)
+    for (int g = 0; g < C::G; ++g) {
+      if (!x.has(g)) continue;
+      if (__ballot(piece[g] == m) != 0) {
 #pragma unroll
         for (int i = 0; i < C::V; ++i) {
           const bool largest = x.at(g, i) == m;
           eq += largest ? 1.f : 0.f;
           add(largest ? -INFINITY : x.at(g, i));
         }
-      eq = wave_reduce<OpAdd>(eq);  // at most 8192: exact
-    } else {
-#pragma unroll
-      for (int g = 0; g < C::G; ++g)
+      } else {
 #pragma unroll
         for (int i = 0; i < C::V; ++i) add(x.at(g, i));
+      }
     }
-    s = wave_reduce<OpAdd>(s);
-    a = wave_reduce<OpAdd>(a) * 0.69314718055994530942f;
+    s = wave_reduce<OpAdd, 1, L>(s);
+    a = wave_reduce<OpAdd, 1, L>(a) * 0.69314718055994530942f;
+    if (__ballot(eq != 0.f) != 0) eq = wave_reduce<OpAdd, 1, L>(eq);  // at most 8192: exact
     if constexpr (W > 1) {
       if (lane == 0) {
         sums[0][wave] = s;
         sums[1][wave] = a;
         sums[2][wave] = eq;
+        counts[wave] = count;
       }
     }
     __syncthreads();
-    const int found = count;
-    if (top_k > 0) {
-      if (m != m || found > kRanked) {
-        const bool listed = m == m && found <= kList;
+    if (KT > 0 && top_k > 0) {
+      int largest = count;
+      if constexpr (W > 1) largest = max(max(counts[0], counts[1]), max(counts[2], counts[3]));
+      if (m != m || largest > kRanked) {
+        const bool listed = m == m && largest <= kList;
         uint64_t last = ~0ull;
         for (int j = 0; j < top_k; ++j) {
           uint64_t best = 0;
           if (listed) {
 #pragma nounroll
-            for (int i = threadIdx.x; i < found; i += C::kThreads) {
+            for (int i = lane; i < count; i += L) {
               const uint64_t key = list[i];
               if (key < last && key > best) best = key;
             }
           } else {
-            const int first = (int)max<int64_t>(c0, 0), end = (int)min<int64_t>(c0 + C::kPieces * C::V, classes);
 #pragma nounroll
-            for (int k = first + threadIdx.x; k < end; k += C::kThreads) {
+            for (int k = k0 + all; k < k0 + x.len; k += L * W) {
               const float v = ld(row + k);
               const uint64_t key = rank_key(v, (uint32_t)k);
               if (!(v == -INFINITY) && key < last && key > best) best = key;
             }
           }
-          best = wave_max_key(best);
+          best = wave_max_key<L>(best);
           if constexpr (W > 1) {
             if (lane == 0) most[j & 1][wave] = best;
             __syncthreads();
             best = max(max(most[j & 1][0], most[j & 1][1]), max(most[j & 1][2], most[j & 1][3]));
           }
           last = best;
-          if (threadIdx.x == 0) top[j] = best;
+          if (all == 0) top[j] = best;
         }
       } else {
-        for (int i = threadIdx.x; i < found; i += C::kThreads) {
+        for (int i = lane; i < count; i += L) {
           const uint64_t own_key = list[i];
           int above = 0;
-          for (int j = 0; j < found; ++j) above += list[j] > own_key;
+          for (int w = 0; w < W; ++w) {
+            const uint64_t* other = W == 1 ? list : lists[w];
+            const int have = W == 1 ? count : counts[w];
+            for (int j = 0; j < have; ++j) above += other[j] > own_key;
+          }
           if (above < top_k) top[above] = own_key;
         }
       }
       __syncthreads();
     }
-    if (wave == 0) {
+    if (wave == 0 && live) {
       if constexpr (W > 1) {
         s = (sums[0][0] + sums[0][1]) + (sums[0][2] + sums[0][3]);
         a = (sums[1][0] + sums[1][1]) + (sums[1][2] + sums[1][3]);
@@ -298,7 +360,7 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
       }
       const Part p{m, m == -INFINITY ? 0.f : s + (eq - 1.f), a};
       if (parts == 1) {
-        write_row(row, r, classes, labels, top_k, p, top, o);
+        write_row(lane, r, lab, top_k, p, top, o);
       } else {
         const int64_t item = r * parts + blockIdx.x;
         if (lane == 0) part_out[item] = make_float4(p.m, p.t, p.a, 0.f);
@@ -310,14 +372,14 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
 }
 
 // Joins the parts of a row, one wavefront per row.  Lane l takes the parts l,
-// l + 64, ..; the best classes come off the heads of 63 of the parts' lists at
-// a time and of the list so far (lane 63).
+// l + 64, ..; the best classes come off the heads of 64 of the parts' lists, or
+// of 63 more and of the list so far (lane 63).
 template <typename T>
 __global__ __launch_bounds__(64) void k_scores_join(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
                                                     int parts, const int32_t* __restrict__ labels, int top_k,
                                                     Outputs o, const float4* __restrict__ part_in,
                                                     const uint64_t* __restrict__ keys_in) {
-  __shared__ uint64_t top[kMaxTop];
+  __shared__ uint64_t list[64 * kMaxTop], top[kMaxTop];
   const int lane = threadIdx.x;
   for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
     Part p{-INFINITY, 0.f, 0.f};
@@ -333,29 +395,26 @@ __global__ __launch_bounds__(64) void k_scores_join(const T* __restrict__ z, int
     if (lane < kMaxTop) top[lane] = 0;
     __syncthreads();
     if (top_k > 0) {
-      for (int c0 = 0; c0 < parts; c0 += 63) {
-        const uint64_t* mine = keys_in + (r * parts + c0 + lane) * top_k;
-        const bool have = lane < 63 && c0 + lane < parts;
-        int at = 0;  // entries taken off this lane's list
-        uint64_t keep = lane < top_k ? top[lane] : 0;  // the list so far
-        uint64_t head = have ? mine[0] : lane == 63 ? top[0] : 0;
+      for (int c0 = 0; c0 < parts;) {
+        const int lists = min(parts - c0, c0 == 0 ? 64 : 63), carry = c0 == 0 ? 0 : 1;
+        const uint64_t* from = keys_in + (r * parts + c0) * top_k;
+        for (int i = lane; i < lists * top_k; i += 64) list[i] = from[i];
+        if (carry && lane < top_k) list[63 * kMaxTop + lane] = top[lane];
         __syncthreads();
+        const uint64_t* mine = lane < lists ? list + lane * top_k : list + 63 * kMaxTop;
+        const bool have = lane < lists || (carry && lane == 63);
+        uint64_t head = have ? mine[0] : 0;
+        int at = 0;  // entries taken off this lane's list
         for (int j = 0; j < top_k; ++j) {
           const uint64_t win = wave_max_key(head);
           if (lane == 0) top[j] = win;
-          const bool took = win != 0 && head == win;
-          const bool old = __ballot(took) >> 63 & 1;  // off the list so far
-          if (took) ++at;
-          const int at63 = __shfl(at, 63, 64);
-          const uint64_t next63 = (uint64_t)__shfl((uint32_t)(keep >> 32), at63 & 63, 64) << 32 |
-                                  __shfl((uint32_t)keep, at63 & 63, 64);
-          if (took && have) head = at < top_k ? mine[at] : 0;
-          if (old && lane == 63) head = at63 < top_k ? next63 : 0;
+          if (win != 0 && head == win) head = ++at < top_k ? mine[at] : 0;
         }
         __syncthreads();
+        c0 += lists;
       }
     }
-    write_row(z + r * ldz, r, classes, labels, top_k, p, top, o);
+    write_row(lane, r, label_of(z + r * ldz, labels, r, classes), top_k, p, top, o);
     __syncthreads();
   }
 }
@@ -365,8 +424,9 @@ __global__ __launch_bounds__(64) void k_scores_join(const T* __restrict__ z, int
 // wavefront reads 64 consecutive rows with 16-byte loads at each row's own
 // alignment (the hardware takes any), a row's loads back to back so that the
 // lines its lanes share are still in the L1.  The KT best are kept sorted by
-// insertion, a strict comparison from the lowest class up (so ties stay in
-// order); the first of them is the row's largest, left out of t.
+// insertion: bf16 as keys that hold the class too, one operation a place (a
+// value, class pair takes four); fp32 by strict comparisons from the lowest
+// class up, so that ties stay in order.  The first is left out of t.
 // Values [AT, AT + N) of the row, N values of at most 16 bytes; -inf past the end.
 template <typename T, int AT, int N, int NC>
 __device__ __forceinline__ void load_span(const T* __restrict__ row, int classes, float (&x)[NC]) {
@@ -398,41 +458,85 @@ __device__ __forceinline__ void load_row(const T* __restrict__ row, int classes,
   }
 }
 
+// The middle of three: where in goes among a >= b, or b, or a shifted down.
+__device__ __forceinline__ int32_t middle(int32_t in, int32_t a, int32_t b) {
+  int32_t r;
+  asm("v_med3_i32 %0, %1, %2, %3" : "=v"(r) : "v"(in), "v"(a), "v"(b));
+  return r;
+}
+
 template <typename T, int NC, int KT>
 __global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
-                                                    const int32_t* __restrict__ labels, int top_k, Outputs o) {
-  const int64_t r = (int64_t)blockIdx.x * 64 + threadIdx.x;
-  if (r >= n) return;
+                                                    const int32_t* __restrict__ labels, int top_k, uint32_t magic,
+                                                    Outputs o) {
+  // the best classes of the 64 rows are 64 top_k consecutive values: they go
+  // out through LDS, each lane's an odd number of words apart
+  constexpr int kStride = KT | 1;
+  __shared__ uint32_t stage[KT > 1 ? 2 : 1][KT > 1 ? 64 * kStride : 1];
+  const int64_t r0 = (int64_t)blockIdx.x * 64;
+  const int rows = (int)min<int64_t>(64, n - r0);
+  const int64_t r = r0 + min((int)threadIdx.x, rows - 1);  // a last lane without a row repeats the last one
+  const bool live = (int)threadIdx.x < rows;
   const T* row = z + r * ldz;
   float x[NC];
   load_row<T, NC>(row, classes, x);
-  const int lab = o.logprob ? labels[r] : -1;
-  float m = -INFINITY, tv[KT];
+  const Label label = label_of(row, labels, r, classes);
+  const int lab = label.k;
+  const float xl = label.x;
+  float m = -INFINITY;  // NaN if the row holds one
+  float tv[KT];
   int ti[KT];
+  if constexpr (sizeof(T) == 2) {
+    // value and class as one whole number: the value's 16 bits so that they
+    // order as a signed number, below them the class, the lowest largest
+    int32_t key[KT];
 #pragma unroll
-  for (int j = 0; j < KT; ++j) {
-    tv[j] = -INFINITY;
-    ti[j] = -1;
-  }
+    for (int j = 0; j < KT; ++j) key[j] = INT32_MIN;
 #pragma unroll
-  for (int k0 = 0; k0 < NC; k0 += 4)
-    if (k0 < classes) {
+    for (int k0 = 0; k0 < NC; k0 += 4)
+      if (k0 < classes) {
 #pragma unroll
-      for (int k = k0; k < k0 + 4; ++k) {
-        const float v = x[k];  // -inf past the end: above nothing
-        m = OpMax::of(m, v);
-        bool above[KT];
+        for (int k = k0; k < k0 + 4; ++k) {
+          m = OpMax::of(m, x[k]);
+          const int32_t bits = (int32_t)__float_as_uint(x[k] + 0.f);  // -0 is 0
+          const int32_t in = (bits ^ ((bits >> 31) & 0x7fff0000)) + (NC - 1 - k);
 #pragma unroll
-        for (int j = 0; j < KT; ++j) above[j] = v > tv[j];
-#pragma unroll
-        for (int j = KT - 1; j >= 0; --j) {
-          const int up = j > 0 ? j - 1 : 0;
-          const bool shift = j > 0 && above[up];
-          tv[j] = shift ? tv[up] : above[j] ? v : tv[j];
-          ti[j] = shift ? ti[up] : above[j] ? k : ti[j];
+          for (int j = KT - 1; j > 0; --j) key[j] = middle(in, key[j - 1], key[j]);
+          key[0] = max(key[0], in);
         }
       }
+#pragma unroll
+    for (int j = 0; j < KT; ++j) {
+      const int32_t top = key[j] & (int32_t)0xffff0000;
+      tv[j] = __uint_as_float((uint32_t)(top ^ ((top >> 31) & 0x7fff0000)));
+      ti[j] = NC - 1 - (key[j] & 0xffff);
     }
+  } else {
+#pragma unroll
+    for (int j = 0; j < KT; ++j) {
+      tv[j] = -INFINITY;
+      ti[j] = -1;
+    }
+#pragma unroll
+    for (int k0 = 0; k0 < NC; k0 += 4)
+      if (k0 < classes) {
+#pragma unroll
+        for (int k = k0; k < k0 + 4; ++k) {
+          const float v = x[k];  // -inf past the end: above nothing
+          m = OpMax::of(m, v);
+          bool above[KT];
+#pragma unroll
+          for (int j = 0; j < KT; ++j) above[j] = v > tv[j];
+#pragma unroll
+          for (int j = KT - 1; j > 0; --j) {
+            ti[j] = above[j - 1] ? ti[j - 1] : above[j] ? k : ti[j];
+            tv[j] = __builtin_amdgcn_fmed3f(v, tv[j - 1], tv[j]);
+          }
+          ti[0] = above[0] ? k : ti[0];
+          tv[0] = fmaxf(tv[0], v);
+        }
+      }
+  }
   Part p{m, 0.f, 0.f};
   const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
@@ -449,97 +553,111 @@ __global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int
     }
   p.a *= 0.69314718055994530942f;
   const float2 lh = finish(p);
-  if (o.logprob) o.logprob[r] = lab < 0 ? 0.f : lab >= classes ? NAN : (ld(row + lab) - base) - lh.x;
-  o.entropy[r] = lh.y;
-  reinterpret_cast<float2*>(o.stats)[r] = make_float2(m, lh.x);
+  if (live) {
+    if (o.logprob) o.logprob[r] = lab < 0 ? 0.f : (xl - base) - lh.x;
+    o.entropy[r] = lh.y;
+    reinterpret_cast<float2*>(o.stats)[r] = make_float2(m, lh.x);
+  }
   if (top_k == 0) return;
   if (m != m) {  // a NaN, which the comparisons passed over: one more pass per class
     uint64_t last = ~0ull;
-    for (int j = 0; j < top_k; ++j) {
-      uint64_t best = 0;
-      for (int k = 0; k < classes; ++k) {
-        const uint64_t key = rank_key(ld(row + k), (uint32_t)k);
-        if (key < last && key > best) best = key;
+#pragma unroll
+    for (int j = 0; j < KT; ++j)
+      if (j < top_k) {
+        uint64_t best = 0;
+#pragma nounroll
+        for (int k = 0; k < classes; ++k) {
+          const uint64_t key = rank_key(ld(row + k), (uint32_t)k);
+          if (key < last && key > best) best = key;
+        }
+        last = best;
+        ti[j] = (int32_t)key_class(best);
+        tv[j] = NAN;
       }
-      last = best;
-      o.top_index[r * top_k + j] = (int32_t)key_class(best);
-      o.top_logprob[r * top_k + j] = NAN;
-    }
-    return;
+  } else if (sizeof(T) == 4) {
+    int fill = 0;  // fewer classes above -inf than asked for: the lowest of the others follow
+#pragma unroll
+    for (int j = 0; j < KT; ++j)
+      if (j < top_k && tv[j] == -INFINITY) {
+        for (bool listed = true; listed;) {
+          listed = false;
+#pragma unroll
+          for (int i = 0; i < KT; ++i) listed |= tv[i] > -INFINITY && ti[i] == fill;
+          fill += listed;
+        }
+        ti[j] = fill++;
+      }
   }
-  int fill = 0;  // fewer classes above -inf than asked for: the lowest of the others follow
-#pragma unroll
-  for (int j = 0; j < KT; ++j)
-    if (j < top_k && tv[j] == -INFINITY) {
-      for (bool listed = true; listed;) {
-        listed = false;
-#pragma unroll
-        for (int i = 0; i < KT; ++i) listed |= tv[i] > -INFINITY && ti[i] == fill;
-        fill += listed;
-      }
-      ti[j] = fill++;
+  if constexpr (KT == 1) {
+    if (live) {
+      o.top_index[r] = ti[0];
+      o.top_logprob[r] = (tv[0] - base) - lh.x;
     }
-  int32_t* ix = o.top_index + r * top_k;
-  float* lp = o.top_logprob + r * top_k;
-  if (top_k == KT) {  // one wide store
-#pragma unroll
-    for (int j = 0; j < KT; ++j) ix[j] = ti[j];
-#pragma unroll
-    for (int j = 0; j < KT; ++j) lp[j] = (tv[j] - base) - lh.x;
   } else {
 #pragma unroll
     for (int j = 0; j < KT; ++j)
       if (j < top_k) {
-        ix[j] = ti[j];
-        lp[j] = (tv[j] - base) - lh.x;
+        stage[0][threadIdx.x * kStride + j] = (uint32_t)ti[j];
+        stage[1][threadIdx.x * kStride + j] = __float_as_uint((tv[j] - base) - lh.x);
       }
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * top_k; i += 64) {
+      const int at = (int)(((uint32_t)i * magic) >> 20);  // i / top_k, exact for i < 1024
+      const int from = at * kStride + (i - at * top_k);
+      o.top_index[r0 * top_k + i] = (int32_t)stage[0][from];
+      o.top_logprob[r0 * top_k + i] = __uint_as_float(stage[1][from]);
+    }
   }
 }
 
-// Which kernel takes a row, by its length alone (and, for rows of several
-// chunks, by how many there are): one workgroup holds up to 64 W E values.
+// Which kernel takes rows of more than kRowMax classes, by their length (and,
+// for rows of several chunks, by how many rows there are): the fewest lanes
+// that hold the row at 32 values each, since what a team does once per row
+// (its reductions, the best classes' ranks) is as much work for 64 values as for 2048.
 struct Route {
-  int waves, per_thread;  // W, E
-  int parts;              // chunks of a row
+  int lanes, per_lane;  // L W, E
+  int parts;            // chunks of a row
 };
 Route route_of(int64_t n, int classes) {
-  // up to 7 values of the first piece may belong to the row before
-  const int64_t len = (int64_t)classes + 7;
-  if (classes <= 510) return {1, 8, 1};     // 4-byte pieces: at most one such value
-  if (len <= 2048) return {4, 8, 1};
-  if (len <= 8192) return {4, 32, 1};
-  // long rows: chunks of 8192 once they are enough workgroups for 256 CUs,
-  // else four times as many
-  const int64_t big = ceil_div(len, 8192);
-  return n * big >= 512 ? Route{4, 32, (int)big} : Route{4, 8, (int)ceil_div(len, 2048)};
+  if (classes <= 512) return {16, 32, 1};
+  if (classes <= 2048) return {64, 32, 1};
+  if (classes <= 8192) return {256, 32, 1};
+  // chunks of 8192 once they are enough workgroups for 256 CUs, else four times as many
+  const int big = (int)ceil_div(classes, 8192);
+  return n * big >= 512 ? Route{256, 32, big} : Route{256, 8, (int)ceil_div(classes, 2048)};
 }
 
-constexpr int kRowMax = 64;  // classes of a row that one thread takes
+// Classes of a row that one thread takes: up to 64, and up to 128 where there
+// are wavefronts of rows for every SIMD.
+constexpr int kRowMax = 64, kRowMaxMany = 128, kManyRows = 1 << 16;
 
 template <typename T, int NC>
 void launch_rows(const T* z, int64_t ldz, int64_t n, int classes, const int32_t* labels, int top_k, const Outputs& o,
                  hipStream_t s) {
   const unsigned g = (unsigned)ceil_div(n, 64);
+  const uint32_t magic = top_k > 0 ? ((1u << 20) + top_k - 1) / top_k : 0;
   if (top_k <= 1)
-    k_scores_rows<T, NC, 1><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o);
+    k_scores_rows<T, NC, 1><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, magic, o);
   else if (top_k <= 3)
-    k_scores_rows<T, NC, 3><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o);
+    k_scores_rows<T, NC, 3><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, magic, o);
   else if (top_k <= 8)
-    k_scores_rows<T, NC, 8><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o);
+    k_scores_rows<T, NC, 8><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, magic, o);
   else
-    k_scores_rows<T, NC, 16><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o);
+    k_scores_rows<T, NC, 16><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, magic, o);
 }
 
 template <typename T>
 sscn_status launch_scores(const T* z, int64_t ldz, int64_t n, int classes, const int32_t* labels, int top_k,
                           const Outputs& o, void* workspace, hipStream_t s) {
-  if (classes <= kRowMax) {
+  if (classes <= kRowMax || (classes <= kRowMaxMany && n >= kManyRows)) {
     if (classes <= 16)
       launch_rows<T, 16>(z, ldz, n, classes, labels, top_k, o, s);
     else if (classes <= 32)
       launch_rows<T, 32>(z, ldz, n, classes, labels, top_k, o, s);
-    else
+    else if (classes <= 64)
       launch_rows<T, 64>(z, ldz, n, classes, labels, top_k, o, s);
+    else
+      launch_rows<T, 128>(z, ldz, n, classes, labels, top_k, o, s);
     SSCN_HIP(hipGetLastError());
     return SSCN_OK;
   }
@@ -548,13 +666,25 @@ sscn_status launch_scores(const T* z, int64_t ldz, int64_t n, int classes, const
   float4* parts = (float4*)workspace;
   uint64_t* keys = (uint64_t*)(parts + items);
   // a workgroup takes rows in turn once there are some 16384 of them
-  const dim3 g((unsigned)w.parts, (unsigned)std::max<int64_t>(1, std::min<int64_t>(n, 16384 / w.parts)));
-  if (w.waves == 1)
-    k_scores_chunk<T, 1, 8><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
-  else if (w.per_thread == 8)
-    k_scores_chunk<T, 4, 8><<<g, 256, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
+  const unsigned by_team = (unsigned)std::min<int64_t>(ceil_div(n, 64 / std::min(w.lanes, 64)), 16384);
+  const dim3 by_part((unsigned)w.parts, (unsigned)std::max<int64_t>(1, std::min<int64_t>(n, 16384 / w.parts)));
+  const auto run = [&](auto kt) {
+    constexpr int KT = decltype(kt)::value;
+    if (w.lanes == 16)
+      k_scores_chunk<T, 16, 1, 32, KT><<<by_team, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
+    else if (w.lanes == 64)
+      k_scores_chunk<T, 64, 1, 32, KT><<<by_team, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
+    else if (w.per_lane == 32)
+      k_scores_chunk<T, 64, 4, 32, KT><<<by_part, 256, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
+    else
+      k_scores_chunk<T, 64, 4, 8, KT><<<by_part, 256, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
+  };
+  if (top_k == 0)
+    run(std::integral_constant<int, 0>{});
+  else if (top_k <= 8)
+    run(std::integral_constant<int, 8>{});
   else
-    k_scores_chunk<T, 4, 32><<<g, 256, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
+    run(std::integral_constant<int, 16>{});
   SSCN_HIP(hipGetLastError());
   if (w.parts > 1) {
     k_scores_join<T><<<(unsigned)std::min<int64_t>(n, 16384), 64, 0, s>>>(z, ldz, n, classes, w.parts, labels, top_k, o,
@@ -667,47 +797,51 @@ __global__ __launch_bounds__(64) void k_grad_rows(const T* __restrict__ z, int64
   }
 }
 
-// Longer rows, a chunk of a row per turn of a workgroup.
-template <typename T, int W, int E>
+// Longer rows, teams and chunks as in k_scores_chunk; each lane has its team's
+// row in its own registers, so nothing is exchanged.
+template <typename T, int L, int W, int E>
 __global__ __launch_bounds__(64 * W) void k_grad_chunk(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
-                                                       int parts, GradInputs q, T* __restrict__ dz, int64_t ldd) {
-  using C = Chunk<T, W, E>;
-  const int64_t total = n * parts;
-  for (int64_t item = blockIdx.x; item < total; item += gridDim.x) {
-    const int64_t r = item / parts;
+                                                       GradInputs q, T* __restrict__ dz, int64_t ldd) {
+  using C = Chunk<T, L * W, E>;
+  constexpr int kTeams = 64 / L;
+  const int team = (threadIdx.x & 63) / L, all = W == 1 ? threadIdx.x & (L - 1) : (int)threadIdx.x;
+  const int64_t rows = W == 1 ? (int64_t)gridDim.x * kTeams : gridDim.y;
+  for (int64_t r0 = W == 1 ? (int64_t)blockIdx.x * kTeams : blockIdx.y; r0 < n; r0 += rows) {
+    const int64_t r = r0 + team;
     const T* row = z + r * ldz;
     T* to = dz + r * ldd;
-    const int64_t c0 = (item - r * parts) * C::kPieces * C::V - C::head(row);
-    C chunk;
-    chunk.load(row, classes, c0);
-    const GradRow w = grad_row(q, r, classes);
+    const int k0 = W == 1 ? 0 : (int)blockIdx.x * C::kValues, len = min(classes - k0, C::kValues);
+    GradRow w;
+    if (r < n) {
+      C x;
+      x.load(row + k0, all, len);
+      w = grad_row(q, r, classes);
 #pragma unroll
-    for (int g = 0; g < C::G; ++g) {
-      float x[C::V];
+      for (int g = 0; g < C::G; ++g) {
+        const int k = (g * L * W + all) * C::V;
+        if (k >= len) continue;
+        float v[C::V];
 #pragma unroll
-      for (int i = 0; i < C::V; ++i) x[i] = grad_dense(w, chunk.at(g, i));
-      const int64_t k0 = c0 + ((int64_t)g * C::kThreads + threadIdx.x) * C::V;
-      if (k0 >= 0 && k0 + C::V <= classes) {  // one store, at whatever alignment it has
-        if constexpr (sizeof(T) == 4) {
-          __builtin_memcpy(to + k0, x, sizeof(T) * C::V);
+        for (int i = 0; i < C::V; ++i) v[i] = grad_dense(w, x.at(g, i));
+        uint32_t b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          b[i] = sizeof(T) == 4 ? __float_as_uint(v[i]) : pack_bf16(v[2 * i % C::V], v[(2 * i + 1) % C::V]);
+        if (k + C::V <= len) {  // one store, at whatever alignment it has
+          __builtin_memcpy(to + k0 + k, b, 16);
         } else {
-          uint32_t v[C::V / 2];
 #pragma unroll
-          for (int i = 0; i < C::V / 2; ++i) v[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-          __builtin_memcpy(to + k0, v, sizeof(T) * C::V);
+          for (int i = 0; i < C::V; ++i)
+            if (x.place(g) + i >= k) st(to + k0 + x.place(g) + i, v[i]);
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < C::V; ++i)
-          if (k0 + i >= 0 && k0 + i < classes) st(to + k0 + i, x[i]);
       }
     }
     __syncthreads();  // the chunk's stores come before those below
-    for (int j = threadIdx.x - 1; j < q.top_k; j += C::kThreads) {
-      const int k = j < 0 ? w.lab : q.top_index[r * q.top_k + j];
-      if (k >= 0 && k < classes && k >= c0 && k < c0 + C::kPieces * C::V)
-        st(to + k, grad_direct(w, ld(row + k), direct_of(q, w, r, k)));
-    }
+    if (r < n)
+      for (int j = all - 1; j < q.top_k; j += L * W) {
+        const int k = j < 0 ? w.lab : q.top_index[r * q.top_k + j];
+        if (k >= k0 && k < k0 + len) st(to + k, grad_direct(w, ld(row + k), direct_of(q, w, r, k)));
+      }
   }
 }
 
@@ -736,12 +870,13 @@ sscn_status launch_grad(const T* z, int64_t ldz, int64_t n, int classes, const G
     launch_grad_rows<T, 32>(z, ldz, n, classes, q, dz, ldd, s);
   } else if (classes <= kRowMax) {
     launch_grad_rows<T, 64>(z, ldz, n, classes, q, dz, ldd, s);
-  } else if (classes <= 510) {
-    k_grad_chunk<T, 1, 8><<<(unsigned)std::min<int64_t>(n, 16384), 64, 0, s>>>(z, ldz, n, classes, 1, q, dz, ldd);
+  } else if (classes <= 512) {
+    k_grad_chunk<T, 16, 1, 32><<<(unsigned)std::min<int64_t>(ceil_div(n, 4), 32768), 64, 0, s>>>(z, ldz, n, classes, q,
+                                                                                                 dz, ldd);
   } else {
-    const int parts = (int)ceil_div((int64_t)classes + 7, 2048);
-    k_grad_chunk<T, 4, 8><<<(unsigned)std::min<int64_t>(n * parts, 16384), 256, 0, s>>>(z, ldz, n, classes, parts, q,
-                                                                                        dz, ldd);
+    const int64_t parts = ceil_div(classes, 2048);
+    const dim3 g((unsigned)parts, (unsigned)std::max<int64_t>(1, std::min<int64_t>(n, 32768 / parts)));
+    k_grad_chunk<T, 64, 4, 8><<<g, 256, 0, s>>>(z, ldz, n, classes, q, dz, ldd);
   }
   SSCN_HIP(hipGetLastError());
   return SSCN_OK;

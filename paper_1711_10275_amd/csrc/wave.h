@@ -45,11 +45,23 @@ __device__ __forceinline__ float wave_reduce(float v) {
   return v;
 }
 
-// The largest of the lanes' 64-bit keys.
+// How many of the other 15 lanes of this lane's row hold an `of` above v.
+template <int N = 1>
+__device__ __forceinline__ int above_in_row(float of, float v) {
+  if constexpr (N == 16) {
+    return 0;
+  } else {
+    constexpr int kRotate = 0x120 + N;  // the value N lanes away
+    return (__uint_as_float(dpp<kRotate>(__float_as_uint(of))) > v ? 1 : 0) + above_in_row<N + 1>(of, v);
+  }
+}
+
+// The largest of the 64-bit keys of L lanes (16 or 64).
 __device__ __forceinline__ uint64_t key_max(uint64_t a, uint32_t lo, uint32_t hi) {
   const uint64_t b = (uint64_t)hi << 32 | lo;
   return a > b ? a : b;
 }
+template <int L = 64>
 __device__ __forceinline__ uint64_t wave_max_key(uint64_t v) {
 #define SSCN_KEY_STEP(C) v = key_max(v, dpp<C>((uint32_t)v), dpp<C>((uint32_t)(v >> 32)))
   SSCN_KEY_STEP(kQuadXor1);
@@ -57,12 +69,12 @@ __device__ __forceinline__ uint64_t wave_max_key(uint64_t v) {
   SSCN_KEY_STEP(kMirror8);
   SSCN_KEY_STEP(kMirror16);
 #undef SSCN_KEY_STEP
-  {
+  if constexpr (L > 16) {
     const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
     const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
     v = key_max((uint64_t)hi[0] << 32 | lo[0], lo[1], hi[1]);
   }
-  {
+  if constexpr (L > 32) {
     const auto lo = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
     const auto hi = __builtin_amdgcn_permlane32_swap((uint32_t)(v >> 32), (uint32_t)(v >> 32), false, false);
     v = key_max((uint64_t)hi[0] << 32 | lo[0], lo[1], hi[1]);
