@@ -98,12 +98,34 @@ __device__ __forceinline__ Part join(const Part& p, const Part& q) {
   // the low part's values, its largest among them, shift by d
   return {OpMax::of(p.m, q.m), hi.t + e * (1.f + lo.t), hi.a + e * (lo.a + (d < -200.f ? -200.f : d) * (1.f + lo.t))};
 }
+// log(1 + t), t >= 0: log(u) t / (u - 1) for u = 1 + t as rounded, in which
+// u's rounding cancels (Goldberg, "What every computer scientist should know
+// about floating-point arithmetic", theorem 4).  Good to 6 half steps.
+__device__ __forceinline__ float log_1p(float t) {
+  const float u = 1.f + t;
+  return u == 1.f ? t : __builtin_amdgcn_logf(u) * 0.69314718055994530942f * (t * __builtin_amdgcn_rcpf(u - 1.f));
+}
 __device__ __forceinline__ float2 finish(const Part& p) {
   if (p.m == INFINITY || p.m != p.m) return make_float2(NAN, NAN);
   if (p.m == -INFINITY) return make_float2(0.f, 0.f);
-  const float l = log1pf(p.t);
-  return make_float2(l, l - p.a / (1.f + p.t));
+  const float l = log_1p(p.t);
+  return make_float2(l, l - p.a * __builtin_amdgcn_rcpf(1.f + p.t));
 }
+
+// Sums of e^(x - m) and e^(x - m) (x - m) as powers of two, h = (x - m) log2(e).
+// h is one rounded product: a term is off by up to 2.25 |x - m| half steps,
+// which its own size e^(x - m) outweighs; forming the product's low part too
+// would cost three more operations a value.
+struct ExpSums {
+  float base, s = 0.f, a = 0.f;
+  __device__ explicit ExpSums(float m) : base(m == -INFINITY ? 0.f : m) {}
+  __device__ __forceinline__ void add(float x) {
+    const float h = fmaxf((x - base) * 1.44269504088896340736f, -300.f);  // 2^-300 is 0: no 0 * inf
+    const float e = __builtin_amdgcn_exp2f(h);
+    s += e;
+    a = fmaf(e, h, a);
+  }
+};
 
 struct Outputs {
   float *logprob, *entropy, *stats;
@@ -267,19 +289,10 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
         }
       }
     }
-    // The sums, of 2^h with h = (x - m) log2(e): the largest are counted and
-    // left out (only pieces that hold one are searched).  h is one rounded
-    // product: a term is off by up to 2.25 |x - m| half steps, which its own
-    // size e^(x - m) outweighs; forming the product's low part too would cost
-    // three more operations a value.
-    float s = 0.f, a = 0.f, eq = 0.f;
-    const float base = m == -INFINITY ? 0.f : m;
-    const auto add = [&](float v) {
-      const float h = fmaxf((v - base) * 1.44269504088896340736f, -300.f);  // 2^-300 is 0
-      const float e = __builtin_amdgcn_exp2f(h);
-      s += e;
-      a = fmaf(e, h, a);
-    };
+    // the sums: the largest are counted and left out (only pieces that hold
+    // one are searched)
+    ExpSums sum(m);
+    float eq = 0.f;
 #pragma unroll
     for (int g = 0; g < C::G; ++g) {
       if (!x.has(g)) continue;
@@ -288,13 +301,14 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
         for (int i = 0; i < C::V; ++i) {
           const bool largest = x.at(g, i) == m;
           eq += largest ? 1.f : 0.f;
-          add(largest ? -INFINITY : x.at(g, i));
+          sum.add(largest ? -INFINITY : x.at(g, i));
         }
       } else {
 #pragma unroll
-        for (int i = 0; i < C::V; ++i) add(x.at(g, i));
+        for (int i = 0; i < C::V; ++i) sum.add(x.at(g, i));
       }
     }
+    float s = sum.s, a = sum.a;
     s = wave_reduce<OpAdd, 1, L>(s);
     a = wave_reduce<OpAdd, 1, L>(a) * 0.69314718055994530942f;
     if (__ballot(eq != 0.f) != 0) eq = wave_reduce<OpAdd, 1, L>(eq);  // at most 8192: exact
@@ -427,34 +441,47 @@ __global__ __launch_bounds__(64) void k_scores_join(const T* __restrict__ z, int
 // insertion: bf16 as keys that hold the class too, one operation a place (a
 // value, class pair takes four); fp32 by strict comparisons from the lowest
 // class up, so that ties stay in order.  The first is left out of t.
-// Values [AT, AT + N) of the row, N values of at most 16 bytes; -inf past the end.
-template <typename T, int AT, int N, int NC>
-__device__ __forceinline__ void load_span(const T* __restrict__ row, int classes, float (&x)[NC]) {
-  if (AT + N <= classes) {
-    if constexpr (N == 1) {
-      x[AT] = ld(row + AT);
-    } else {
-      uint32_t w[N * sizeof(T) / 4];
-      __builtin_memcpy(w, row + AT, N * sizeof(T));
+// A row of more than NP and at most NC classes as fp32, -inf past its end, in
+// pieces of 16 bytes.  A cut last piece runs into what follows the row (and is
+// cut off below); where that is the end of the matrix, `last`, pieces are moved
+// back into it, and those few rows read again value by value.  There is no
+// branch between the loads: around one the compiler waits for it before the
+// next goes out.
+template <typename T, int NP, int NC>
+__device__ __forceinline__ void load_row(const T* __restrict__ row, const T* __restrict__ last, bool one_piece,
+                                         int classes, float (&x)[NC]) {
+  constexpr int V = 16 / (int)sizeof(T);
+  uint32_t w[NC / V][4];
+  const int room = (int)min<int64_t>(last - row, NC) - V;  // start of the last piece that fits
+  if (one_piece) {                                         // the matrix holds one: the same for every row
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        x[AT + i] = sizeof(T) == 4 ? __uint_as_float(w[i])
-                    : i % 2        ? __uint_as_float(w[i / 2] & 0xffff0000u)
-                                   : __uint_as_float(w[i / 2] << 16);
+    for (int p = 0; p < NC / V; ++p) __builtin_memcpy(w[p], row + min(p * V, room), 16);
+  }
+  if (!one_piece || room < (classes - 1) / V * V) {
+#pragma unroll
+    for (int p = 0; p < NC / V; ++p) {
+      T one[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) one[i] = row[min(p * V + i, classes - 1)];
+      __builtin_memcpy(w[p], one, 16);
+      asm volatile("" ::: "memory");  // one piece's addresses at a time: all of them took up to 70 registers
     }
-  } else if constexpr (N > 1) {
-    load_span<T, AT, N / 2>(row, classes, x);
-    load_span<T, AT + N / 2, N / 2>(row, classes, x);
-  } else {
-    x[AT] = -INFINITY;
+  }
+#pragma unroll
+  for (int k = 0; k < NC; ++k) {
+    const uint32_t word = sizeof(T) == 4 ? w[k / V][k % V] : w[k / V][k % V / 2];
+    x[k] = __uint_as_float(sizeof(T) == 4 ? word : k % 2 ? word & 0xffff0000u : word << 16);
+    if (k > NP) x[k] = k < classes ? x[k] : -INFINITY;
   }
 }
-template <typename T, int NC, int AT = 0>
-__device__ __forceinline__ void load_row(const T* __restrict__ row, int classes, float (&x)[NC]) {
-  constexpr int V = 16 / (int)sizeof(T);
-  if constexpr (AT < NC) {
-    load_span<T, AT, V>(row, classes, x);
-    load_row<T, NC, AT + V>(row, classes, x);
+
+// f(0), f(4), .. below NC and the number of classes, unrolled for certain (the
+// row's registers have no other index): f gets the group's first class.
+template <int NP, int NC, int K0 = 0, class F>
+__device__ __forceinline__ void groups_of_4(int classes, const F& f) {
+  if constexpr (K0 < NC) {
+    if (K0 <= NP || K0 < classes) f(std::integral_constant<int, K0>{});
+    groups_of_4<NP, NC, K0 + 4>(classes, f);
   }
 }
 
@@ -465,7 +492,7 @@ __device__ __forceinline__ int32_t middle(int32_t in, int32_t a, int32_t b) {
   return r;
 }
 
-template <typename T, int NC, int KT>
+template <typename T, int NP, int NC, int KT>
 __global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
                                                     const int32_t* __restrict__ labels, int top_k, uint32_t magic,
                                                     Outputs o) {
@@ -479,7 +506,7 @@ __global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int
   const bool live = (int)threadIdx.x < rows;
   const T* row = z + r * ldz;
   float x[NC];
-  load_row<T, NC>(row, classes, x);
+  load_row<T, NP, NC>(row, z + (n - 1) * ldz + classes, (n - 1) * ldz + classes >= 16 / (int)sizeof(T), classes, x);
   const Label label = label_of(row, labels, r, classes);
   const int lab = label.k;
   const float xl = label.x;
@@ -492,11 +519,9 @@ __global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int
     int32_t key[KT];
 #pragma unroll
     for (int j = 0; j < KT; ++j) key[j] = INT32_MIN;
+    groups_of_4<NP, NC>(classes, [&](auto k0) {
 #pragma unroll
-    for (int k0 = 0; k0 < NC; k0 += 4)
-      if (k0 < classes) {
-#pragma unroll
-        for (int k = k0; k < k0 + 4; ++k) {
+      for (int k = k0; k < k0 + 4; ++k) {
           m = OpMax::of(m, x[k]);
           const int32_t bits = (int32_t)__float_as_uint(x[k] + 0.f);  // -0 is 0
           const int32_t in = (bits ^ ((bits >> 31) & 0x7fff0000)) + (NC - 1 - k);
@@ -504,7 +529,7 @@ __global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int
           for (int j = KT - 1; j > 0; --j) key[j] = middle(in, key[j - 1], key[j]);
           key[0] = max(key[0], in);
         }
-      }
+    });
 #pragma unroll
     for (int j = 0; j < KT; ++j) {
       const int32_t top = key[j] & (int32_t)0xffff0000;
@@ -517,11 +542,9 @@ __global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int
       tv[j] = -INFINITY;
       ti[j] = -1;
     }
+    groups_of_4<NP, NC>(classes, [&](auto k0) {
 #pragma unroll
-    for (int k0 = 0; k0 < NC; k0 += 4)
-      if (k0 < classes) {
-#pragma unroll
-        for (int k = k0; k < k0 + 4; ++k) {
+      for (int k = k0; k < k0 + 4; ++k) {
           const float v = x[k];  // -inf past the end: above nothing
           m = OpMax::of(m, v);
           bool above[KT];
@@ -535,23 +558,15 @@ __global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int
           ti[0] = above[0] ? k : ti[0];
           tv[0] = fmaxf(tv[0], v);
         }
-      }
+    });
   }
-  Part p{m, 0.f, 0.f};
-  const float base = m == -INFINITY ? 0.f : m;
+  ExpSums sum(m);
+  const float base = sum.base;
+  groups_of_4<NP, NC>(classes, [&](auto k0) {
 #pragma unroll
-  for (int k0 = 0; k0 < NC; k0 += 4)
-    if (k0 < classes) {
-#pragma unroll
-      for (int k = k0; k < k0 + 4; ++k) {
-        // 2^h, as in k_scores_chunk
-        const float h = fmaxf(k == ti[0] ? -INFINITY : (x[k] - base) * 1.44269504088896340736f, -300.f);
-        const float e = __builtin_amdgcn_exp2f(h);
-        p.t += e;
-        p.a = fmaf(e, h, p.a);
-      }
-    }
-  p.a *= 0.69314718055994530942f;
+    for (int k = k0; k < k0 + 4; ++k) sum.add(k == ti[0] ? -INFINITY : x[k]);
+  });
+  const Part p{m, sum.s, sum.a * 0.69314718055994530942f};
   const float2 lh = finish(p);
   if (live) {
     if (o.logprob) o.logprob[r] = lab < 0 ? 0.f : (xl - base) - lh.x;
@@ -627,37 +642,50 @@ Route route_of(int64_t n, int classes) {
   return n * big >= 512 ? Route{256, 32, big} : Route{256, 8, (int)ceil_div(classes, 2048)};
 }
 
-// Classes of a row that one thread takes: up to 64, and up to 128 where there
-// are wavefronts of rows for every SIMD.
-constexpr int kRowMax = 64, kRowMaxMany = 128, kManyRows = 1 << 16;
+// Whether one thread takes a row: of up to 64 classes; up to 128 in bf16, whose
+// best classes cost a thread less, and in fp32 where there are several
+// wavefronts of rows for every SIMD.  (16,383 x 70 bf16, best 8: 12 us by teams
+// of lanes; 65,536 x 128 fp32, best 8: 21 us by teams, 24 by threads; 600,000 x
+// 128: 194 and 117.)
+constexpr int kRowMax = 64;
+template <typename T>
+bool by_thread(int64_t n, int classes) {
+  return classes <= kRowMax || (classes <= 128 && (sizeof(T) == 2 || n >= 1 << 18));
+}
 
-template <typename T, int NC>
+// f(NP, NC) for rows of more than NP and at most NC classes.
+template <class F>
+void by_classes(int classes, const F& f) {
+  if (classes <= 16) f(std::integral_constant<int, 0>{}, std::integral_constant<int, 16>{});
+  else if (classes <= 24) f(std::integral_constant<int, 16>{}, std::integral_constant<int, 24>{});
+  else if (classes <= 32) f(std::integral_constant<int, 24>{}, std::integral_constant<int, 32>{});
+  else if (classes <= 48) f(std::integral_constant<int, 32>{}, std::integral_constant<int, 48>{});
+  else if (classes <= 64) f(std::integral_constant<int, 48>{}, std::integral_constant<int, 64>{});
+  else f(std::integral_constant<int, 64>{}, std::integral_constant<int, 128>{});
+}
+
+template <typename T, int NP, int NC>
 void launch_rows(const T* z, int64_t ldz, int64_t n, int classes, const int32_t* labels, int top_k, const Outputs& o,
                  hipStream_t s) {
   const unsigned g = (unsigned)ceil_div(n, 64);
   const uint32_t magic = top_k > 0 ? ((1u << 20) + top_k - 1) / top_k : 0;
   if (top_k <= 1)
-    k_scores_rows<T, NC, 1><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, magic, o);
+    k_scores_rows<T, NP, NC, 1><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, magic, o);
   else if (top_k <= 3)
-    k_scores_rows<T, NC, 3><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, magic, o);
+    k_scores_rows<T, NP, NC, 3><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, magic, o);
   else if (top_k <= 8)
-    k_scores_rows<T, NC, 8><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, magic, o);
+    k_scores_rows<T, NP, NC, 8><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, magic, o);
   else
-    k_scores_rows<T, NC, 16><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, magic, o);
+    k_scores_rows<T, NP, NC, 16><<<g, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, magic, o);
 }
 
 template <typename T>
 sscn_status launch_scores(const T* z, int64_t ldz, int64_t n, int classes, const int32_t* labels, int top_k,
                           const Outputs& o, void* workspace, hipStream_t s) {
-  if (classes <= kRowMax || (classes <= kRowMaxMany && n >= kManyRows)) {
-    if (classes <= 16)
-      launch_rows<T, 16>(z, ldz, n, classes, labels, top_k, o, s);
-    else if (classes <= 32)
-      launch_rows<T, 32>(z, ldz, n, classes, labels, top_k, o, s);
-    else if (classes <= 64)
-      launch_rows<T, 64>(z, ldz, n, classes, labels, top_k, o, s);
-    else
-      launch_rows<T, 128>(z, ldz, n, classes, labels, top_k, o, s);
+  if (by_thread<T>(n, classes)) {
+    by_classes(classes, [&](auto np, auto nc) {
+      launch_rows<T, decltype(np)::value, decltype(nc)::value>(z, ldz, n, classes, labels, top_k, o, s);
+    });
     SSCN_HIP(hipGetLastError());
     return SSCN_OK;
   }
@@ -753,7 +781,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {  // nearest 
 // Short rows, a thread per row as in k_scores_rows.  The 64 rows of a
 // wavefront go out through LDS, rows an odd number of words apart (each lane
 // its own bank), as consecutive words of 4 bytes (WORDS) or single values.
-template <typename T, int NC, bool WORDS>
+template <typename T, int NP, int NC, bool WORDS>
 __global__ __launch_bounds__(64) void k_grad_rows(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
                                                   GradInputs q, T* __restrict__ dz, int64_t ldd, int stride,
                                                   uint32_t magic) {
@@ -763,21 +791,19 @@ __global__ __launch_bounds__(64) void k_grad_rows(const T* __restrict__ z, int64
   if (r < n) {
     const T* row = z + r * ldz;
     float x[NC];
-    load_row<T, NC>(row, classes, x);
+    load_row<T, NP, NC>(row, z + (n - 1) * ldz + classes, (n - 1) * ldz + classes >= 16 / (int)sizeof(T), classes, x);
     const GradRow w = grad_row(q, r, classes);
+    groups_of_4<NP, NC>(classes, [&](auto k0) {
 #pragma unroll
-    for (int k0 = 0; k0 < NC; k0 += 4)
-      if (k0 < classes) {
-#pragma unroll
-        for (int k = k0; k < k0 + 4; ++k) x[k] = grad_dense(w, x[k]);
-        // whole words: the stride has room for a last group's unused values
-        if constexpr (sizeof(T) == 4) {
-          __builtin_memcpy(out + k0, x + k0, 16);
-        } else {
-          const uint32_t v[2] = {pack_bf16(x[k0], x[k0 + 1]), pack_bf16(x[k0 + 2], x[k0 + 3])};
-          __builtin_memcpy(out + k0, v, 8);
-        }
+      for (int k = k0; k < k0 + 4; ++k) x[k] = grad_dense(w, x[k]);
+      // whole words: the stride has room for a last group's unused values
+      if constexpr (sizeof(T) == 4) {
+        __builtin_memcpy(out + k0, x + k0, 16);
+      } else {
+        const uint32_t v[2] = {pack_bf16(x[k0], x[k0 + 1]), pack_bf16(x[k0 + 2], x[k0 + 3])};
+        __builtin_memcpy(out + k0, v, 8);
       }
+    });
     if (w.lab >= 0 && w.lab < classes) st(out + w.lab, grad_direct(w, ld(row + w.lab), direct_of(q, w, r, w.lab)));
     for (int j = 0; j < q.top_k; ++j) {
       const int k = q.top_index[r * q.top_k + j];
@@ -845,7 +871,7 @@ __global__ __launch_bounds__(64 * W) void k_grad_chunk(const T* __restrict__ z, 
   }
 }
 
-template <typename T, int NC>
+template <typename T, int NP, int NC>
 void launch_grad_rows(const T* z, int64_t ldz, int64_t n, int classes, const GradInputs& q, T* dz, int64_t ldd,
                       hipStream_t s) {
   const int bytes = (int)sizeof(T) * classes;
@@ -856,20 +882,19 @@ void launch_grad_rows(const T* z, int64_t ldz, int64_t n, int classes, const Gra
   const unsigned g = (unsigned)ceil_div(n, 64);
   const size_t lds = (size_t)64 * stride * 4;
   if (words)
-    k_grad_rows<T, NC, true><<<g, 64, lds, s>>>(z, ldz, n, classes, q, dz, ldd, stride, magic);
+    k_grad_rows<T, NP, NC, true><<<g, 64, lds, s>>>(z, ldz, n, classes, q, dz, ldd, stride, magic);
   else
-    k_grad_rows<T, NC, false><<<g, 64, lds, s>>>(z, ldz, n, classes, q, dz, ldd, stride, magic);
+    k_grad_rows<T, NP, NC, false><<<g, 64, lds, s>>>(z, ldz, n, classes, q, dz, ldd, stride, magic);
 }
 
 template <typename T>
 sscn_status launch_grad(const T* z, int64_t ldz, int64_t n, int classes, const GradInputs& q, T* dz, int64_t ldd,
                         hipStream_t s) {
-  if (classes <= 16) {
-    launch_grad_rows<T, 16>(z, ldz, n, classes, q, dz, ldd, s);
-  } else if (classes <= 32) {
-    launch_grad_rows<T, 32>(z, ldz, n, classes, q, dz, ldd, s);
-  } else if (classes <= kRowMax) {
-    launch_grad_rows<T, 64>(z, ldz, n, classes, q, dz, ldd, s);
+  if (classes <= kRowMax) {
+    by_classes(classes, [&](auto np, auto nc) {
+      if constexpr (decltype(nc)::value <= kRowMax)
+        launch_grad_rows<T, decltype(np)::value, decltype(nc)::value>(z, ldz, n, classes, q, dz, ldd, s);
+    });
   } else if (classes <= 512) {
     k_grad_chunk<T, 16, 1, 32><<<(unsigned)std::min<int64_t>(ceil_div(n, 4), 32768), 64, 0, s>>>(z, ldz, n, classes, q,
                                                                                                  dz, ldd);
