@@ -50,7 +50,9 @@ struct Chunk {
   static constexpr int kValues = L * E;
 
   uint32_t w[G][4];  // bf16 two to a word
-  int lane, len;     // lane of the team; values of the chunk, V <= len <= kValues
+  // Lane of the team; values of the chunk, at most kValues.  (A chunk of fewer
+  // than V is a row's last, and its one piece starts in the chunk before.)
+  int lane, len;
 
   // Whether the g-th pieces hold anything: the same for the whole team.
   __device__ bool has(int g) const { return g * kSpan < len; }
@@ -741,7 +743,8 @@ struct GradRow {
   int lab;
   bool empty;
 };
-__device__ __forceinline__ GradRow grad_row(const GradInputs& q, int64_t r, int classes) {
+// direct: the sum of the row's dtop.
+__device__ __forceinline__ GradRow grad_row(const GradInputs& q, int64_t r, int classes, float direct) {
   GradRow w;
   const float2 st = reinterpret_cast<const float2*>(q.stats)[r];
   w.L = st.y;
@@ -751,8 +754,7 @@ __device__ __forceinline__ GradRow grad_row(const GradInputs& q, int64_t r, int 
   w.H = q.dentropy ? q.entropy[r] : 0.f;
   w.lab = q.dlogprob ? q.labels[r] : -1;
   w.g = w.lab < 0 ? 0.f : w.lab >= classes ? NAN : q.dlogprob[r];
-  w.G = w.g;
-  for (int j = 0; j < q.top_k; ++j) w.G += q.dtop[r * q.top_k + j];
+  w.G = w.g + direct;
   if (w.L != w.L) w.G = NAN;  // the clamp below would lose it
   if (w.empty) w.g = w.G = w.h = 0.f;
   return w;
@@ -762,16 +764,10 @@ __device__ __forceinline__ float grad_dense(const GradRow& w, float x) {
   return -__builtin_amdgcn_exp2f(lp * 1.44269504088896340736f) * fmaf(w.h, lp + w.H, w.G);
 }
 __device__ __forceinline__ float grad_direct(const GradRow& w, float x, float A) {
+  if (w.empty) return 0.f;
   const float lp = (x - w.base) - w.L, p = expf(lp);
   return -A * expm1f(lp) - p * ((w.G - A) + (p == 0.f ? 0.f : w.h * (lp + w.H)));
 }
-// What class k receives directly.
-__device__ __forceinline__ float direct_of(const GradInputs& q, const GradRow& w, int64_t r, int k) {
-  float A = k == w.lab ? w.g : 0.f;
-  for (int j = 0; j < q.top_k; ++j) A += q.top_index[r * q.top_k + j] == k ? q.dtop[r * q.top_k + j] : 0.f;
-  return w.empty ? 0.f : A;
-}
-
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {  // nearest even, NaN kept
   typedef __bf16 B2 __attribute__((ext_vector_type(2)));
   typedef float F2 __attribute__((ext_vector_type(2)));
@@ -781,93 +777,144 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {  // nearest 
 // Short rows, a thread per row as in k_scores_rows.  The 64 rows of a
 // wavefront go out through LDS, rows an odd number of words apart (each lane
 // its own bank), as consecutive words of 4 bytes (WORDS) or single values.
-template <typename T, int NP, int NC, bool WORDS>
+// KT: at least top_k; the rows' best classes and their gradients come in
+// through LDS the same way.
+template <typename T, int NP, int NC, bool WORDS, int KT>
 __global__ __launch_bounds__(64) void k_grad_rows(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
                                                   GradInputs q, T* __restrict__ dz, int64_t ldd, int stride,
-                                                  uint32_t magic) {
+                                                  uint32_t magic, uint32_t top_magic) {
   extern __shared__ uint32_t lds[];
-  const int64_t r0 = (int64_t)blockIdx.x * 64, r = r0 + threadIdx.x;
+  constexpr int kStride = KT | 1;
+  __shared__ uint32_t stage[KT ? 2 : 1][KT ? 64 * kStride : 1];
+  const int64_t r0 = (int64_t)blockIdx.x * 64;
+  const int rows = (int)min<int64_t>(64, n - r0);
+  const int64_t r = r0 + min((int)threadIdx.x, rows - 1);  // a last lane without a row repeats the last one
   T* out = reinterpret_cast<T*>(lds + threadIdx.x * stride);
-  if (r < n) {
-    const T* row = z + r * ldz;
-    float x[NC];
-    load_row<T, NP, NC>(row, z + (n - 1) * ldz + classes, (n - 1) * ldz + classes >= 16 / (int)sizeof(T), classes, x);
-    const GradRow w = grad_row(q, r, classes);
-    groups_of_4<NP, NC>(classes, [&](auto k0) {
+  const T* row = z + r * ldz;
+  float x[NC];
+  load_row<T, NP, NC>(row, z + (n - 1) * ldz + classes, (n - 1) * ldz + classes >= 16 / (int)sizeof(T), classes, x);
+  int ti[KT ? KT : 1];
+  float tv[KT ? KT : 1], direct = 0.f;
+  if constexpr (KT > 0) {
+    for (int i = threadIdx.x; i < rows * q.top_k; i += 64) {
+      const int at = (int)(((uint32_t)i * top_magic) >> 20);  // i / top_k, exact for i < 1024
+      const int to = at * kStride + (i - at * q.top_k);
+      stage[0][to] = (uint32_t)q.top_index[r0 * q.top_k + i];
+      stage[1][to] = __float_as_uint(q.dtop[r0 * q.top_k + i]);
+    }
+    __syncthreads();
+    const int mine = min((int)threadIdx.x, rows - 1) * kStride;
 #pragma unroll
-      for (int k = k0; k < k0 + 4; ++k) x[k] = grad_dense(w, x[k]);
-      // whole words: the stride has room for a last group's unused values
-      if constexpr (sizeof(T) == 4) {
-        __builtin_memcpy(out + k0, x + k0, 16);
-      } else {
-        const uint32_t v[2] = {pack_bf16(x[k0], x[k0 + 1]), pack_bf16(x[k0 + 2], x[k0 + 3])};
-        __builtin_memcpy(out + k0, v, 8);
-      }
-    });
-    if (w.lab >= 0 && w.lab < classes) st(out + w.lab, grad_direct(w, ld(row + w.lab), direct_of(q, w, r, w.lab)));
-    for (int j = 0; j < q.top_k; ++j) {
-      const int k = q.top_index[r * q.top_k + j];
-      if (k >= 0 && k < classes) st(out + k, grad_direct(w, ld(row + k), direct_of(q, w, r, k)));
+    for (int j = 0; j < KT; ++j) {
+      ti[j] = j < q.top_k ? (int)stage[0][mine + j] : -1;
+      tv[j] = j < q.top_k ? __uint_as_float(stage[1][mine + j]) : 0.f;
+      direct += tv[j];
     }
   }
+  const GradRow w = grad_row(q, r, classes, direct);
+  groups_of_4<NP, NC>(classes, [&](auto k0) {
+#pragma unroll
+    for (int k = k0; k < k0 + 4; ++k) x[k] = grad_dense(w, x[k]);
+    // whole words: the stride has room for a last group's unused values
+    if constexpr (sizeof(T) == 4) {
+      __builtin_memcpy(out + k0, x + k0, 16);
+    } else {
+      const uint32_t v[2] = {pack_bf16(x[k0], x[k0 + 1]), pack_bf16(x[k0 + 2], x[k0 + 3])};
+      __builtin_memcpy(out + k0, v, 8);
+    }
+  });
+  if (w.lab >= 0 && w.lab < classes) {
+    float A = w.g;
+#pragma unroll
+    for (int j = 0; j < KT; ++j) A += ti[j] == w.lab ? tv[j] : 0.f;
+    st(out + w.lab, grad_direct(w, ld(row + w.lab), A));
+  }
+  if constexpr (KT > 0) {
+#pragma unroll
+    for (int i = 0; i < KT; ++i)
+      if (ti[i] >= 0 && ti[i] < classes) {
+        float A = ti[i] == w.lab ? w.g : 0.f;
+#pragma unroll
+        for (int j = 0; j < KT; ++j) A += ti[j] == ti[i] ? tv[j] : 0.f;
+        st(out + ti[i], grad_direct(w, ld(row + ti[i]), A));
+      }
+  }
   __syncthreads();
-  const int rows = (int)min<int64_t>(64, n - r0);
   const int per = WORDS ? classes * (int)sizeof(T) / 4 : classes;  // items of a row
   for (int i = threadIdx.x; i < rows * per; i += 64) {
-    const int row = (int)(((uint32_t)i * magic) >> 20), at = i - row * per;  // i / per, exact for i < 4096
-    T* to = dz + (r0 + row) * ldd;
+    const int at_row = (int)(((uint32_t)i * magic) >> 20), at = i - at_row * per;  // i / per, exact for i < 4096
+    T* to = dz + (r0 + at_row) * ldd;
     if constexpr (WORDS)
-      reinterpret_cast<uint32_t*>(to)[at] = lds[row * stride + at];
+      reinterpret_cast<uint32_t*>(to)[at] = lds[at_row * stride + at];
     else
-      to[at] = reinterpret_cast<const T*>(lds + row * stride)[at];
+      to[at] = reinterpret_cast<const T*>(lds + at_row * stride)[at];
   }
 }
 
-// Longer rows, teams and chunks as in k_scores_chunk; each lane has its team's
-// row in its own registers, so nothing is exchanged.
-template <typename T, int L, int W, int E>
+// Longer rows, teams as in k_scores_chunk, `span` values of a row to a team;
+// nothing is kept, so a team walks its span piece by piece.  Every 16 lanes
+// hold the row's best classes and their gradients, one a lane.
+template <typename T, int L, int W>
 __global__ __launch_bounds__(64 * W) void k_grad_chunk(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
-                                                       GradInputs q, T* __restrict__ dz, int64_t ldd) {
-  using C = Chunk<T, L * W, E>;
-  constexpr int kTeams = 64 / L;
+                                                       int span, GradInputs q, T* __restrict__ dz, int64_t ldd) {
+  constexpr int V = 16 / (int)sizeof(T), kTeams = 64 / L;
   const int team = (threadIdx.x & 63) / L, all = W == 1 ? threadIdx.x & (L - 1) : (int)threadIdx.x;
   const int64_t rows = W == 1 ? (int64_t)gridDim.x * kTeams : gridDim.y;
+  const int k0 = W == 1 ? 0 : (int)blockIdx.x * span, len = min(classes - k0, span);
   for (int64_t r0 = W == 1 ? (int64_t)blockIdx.x * kTeams : blockIdx.y; r0 < n; r0 += rows) {
     const int64_t r = r0 + team;
     const T* row = z + r * ldz;
     T* to = dz + r * ldd;
-    const int k0 = W == 1 ? 0 : (int)blockIdx.x * C::kValues, len = min(classes - k0, C::kValues);
-    GradRow w;
+    constexpr int G = 2, kStep = L * W * V;  // pieces in flight
+    uint32_t b[G][4];
+    const int first = all * V;
+    const auto load = [&](int kb) {
+#pragma unroll
+      for (int g = 0; g < G; ++g)  // a cut piece is the V values up to the span's end
+        __builtin_memcpy(b[g], row + k0 + min(kb + g * kStep, len - V), 16);
+    };
+    if (r < n) load(first);  // before what the row's numbers wait for
+    GradRow w{};
+    const int j = threadIdx.x & 15;
+    const bool has = r < n && j < q.top_k;
+    const int cls = has ? q.top_index[r * q.top_k + j] : -1;
+    const float t = has ? q.dtop[r * q.top_k + j] : 0.f;
     if (r < n) {
-      C x;
-      x.load(row + k0, all, len);
-      w = grad_row(q, r, classes);
+      w = grad_row(q, r, classes, wave_reduce<OpAdd, 1, 16>(t));
+      for (int kb = first; kb < len;) {
 #pragma unroll
-      for (int g = 0; g < C::G; ++g) {
-        const int k = (g * L * W + all) * C::V;
-        if (k >= len) continue;
-        float v[C::V];
+        for (int g = 0; g < G; ++g) {
+          const int k = kb + g * kStep, at = k0 + min(k, len - V);
+          if (k >= len) break;
+          float v[V];
 #pragma unroll
-        for (int i = 0; i < C::V; ++i) v[i] = grad_dense(w, x.at(g, i));
-        uint32_t b[4];
+          for (int i = 0; i < V; ++i)
+            v[i] = grad_dense(w, sizeof(T) == 4 ? __uint_as_float(b[g][i % 4])
+                                 : i % 2        ? __uint_as_float(b[g][i / 2] & 0xffff0000u)
+                                                : __uint_as_float(b[g][i / 2] << 16));
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          b[i] = sizeof(T) == 4 ? __float_as_uint(v[i]) : pack_bf16(v[2 * i % C::V], v[(2 * i + 1) % C::V]);
-        if (k + C::V <= len) {  // one store, at whatever alignment it has
-          __builtin_memcpy(to + k0 + k, b, 16);
-        } else {
+          for (int i = 0; i < 4; ++i)
+            b[g][i] = sizeof(T) == 4 ? __float_as_uint(v[i]) : pack_bf16(v[2 * i % V], v[(2 * i + 1) % V]);
+          if (k + V <= len) {  // one store, at whatever alignment it has
+            __builtin_memcpy(to + at, b[g], 16);
+          } else {
 #pragma unroll
-          for (int i = 0; i < C::V; ++i)
-            if (x.place(g) + i >= k) st(to + k0 + x.place(g) + i, v[i]);
+            for (int i = 0; i < V; ++i)
+              if (at + i >= k0 + k) st(to + at + i, v[i]);
+          }
         }
+        kb += G * kStep;
+        if (kb < len) load(kb);
       }
     }
-    __syncthreads();  // the chunk's stores come before those below
-    if (r < n)
-      for (int j = all - 1; j < q.top_k; j += L * W) {
-        const int k = j < 0 ? w.lab : q.top_index[r * q.top_k + j];
-        if (k >= k0 && k < k0 + len) st(to + k, grad_direct(w, ld(row + k), direct_of(q, w, r, k)));
-      }
+    __syncthreads();  // the team's stores come before those below
+    const bool mine = cls >= k0 && cls < k0 + len, label_here = r < n && w.lab >= k0 && w.lab < k0 + len;
+    if (all < 16 && __ballot(mine || label_here) != 0) {
+      const Same same = same_in_row(cls, t);
+      const float A = t + same.sum, to_label = w.g + wave_reduce<OpAdd, 1, 16>(cls == w.lab ? t : 0.f);
+      if (mine && cls != w.lab && !same.before) st(to + cls, grad_direct(w, ld(row + cls), A));
+      if (label_here && all == 0) st(to + w.lab, grad_direct(w, ld(row + w.lab), to_label));
+    }
   }
 }
 
@@ -879,12 +926,20 @@ void launch_grad_rows(const T* z, int64_t ldz, int64_t n, int classes, const Gra
   const int stride = (int)(ceil_div(classes, 4) * 4 * sizeof(T) / 4) | 1;
   const int per = words ? bytes / 4 : classes;
   const uint32_t magic = ((1u << 20) + per - 1) / per;
+  const uint32_t top_magic = q.top_k > 0 ? ((1u << 20) + q.top_k - 1) / q.top_k : 0;
   const unsigned g = (unsigned)ceil_div(n, 64);
   const size_t lds = (size_t)64 * stride * 4;
-  if (words)
-    k_grad_rows<T, NP, NC, true><<<g, 64, lds, s>>>(z, ldz, n, classes, q, dz, ldd, stride, magic);
-  else
-    k_grad_rows<T, NP, NC, false><<<g, 64, lds, s>>>(z, ldz, n, classes, q, dz, ldd, stride, magic);
+  const auto run = [&](auto words_t) {
+    constexpr bool WORDS = decltype(words_t)::value;
+    if (q.top_k == 0)
+      k_grad_rows<T, NP, NC, WORDS, 0><<<g, 64, lds, s>>>(z, ldz, n, classes, q, dz, ldd, stride, magic, top_magic);
+    else if (q.top_k <= 4)
+      k_grad_rows<T, NP, NC, WORDS, 4><<<g, 64, lds, s>>>(z, ldz, n, classes, q, dz, ldd, stride, magic, top_magic);
+    else
+      k_grad_rows<T, NP, NC, WORDS, 16><<<g, 64, lds, s>>>(z, ldz, n, classes, q, dz, ldd, stride, magic, top_magic);
+  };
+  if (words) run(std::true_type{});
+  else run(std::false_type{});
 }
 
 template <typename T>
@@ -896,12 +951,15 @@ sscn_status launch_grad(const T* z, int64_t ldz, int64_t n, int classes, const G
         launch_grad_rows<T, decltype(np)::value, decltype(nc)::value>(z, ldz, n, classes, q, dz, ldd, s);
     });
   } else if (classes <= 512) {
-    k_grad_chunk<T, 16, 1, 32><<<(unsigned)std::min<int64_t>(ceil_div(n, 4), 32768), 64, 0, s>>>(z, ldz, n, classes, q,
-                                                                                                 dz, ldd);
+    k_grad_chunk<T, 16, 1><<<(unsigned)std::min<int64_t>(ceil_div(n, 4), 32768), 64, 0, s>>>(z, ldz, n, classes, 512, q,
+                                                                                             dz, ldd);
+  } else if (classes <= 2048) {
+    k_grad_chunk<T, 64, 1><<<(unsigned)std::min<int64_t>(n, 32768), 64, 0, s>>>(z, ldz, n, classes, 2048, q, dz, ldd);
   } else {
-    const int64_t parts = ceil_div(classes, 2048);
+    const int span = 2048;  // (8192, with a quarter of the workgroups: 78 us for 69 at 1024 x 40001 fp32)
+    const int64_t parts = ceil_div(classes, span);
     const dim3 g((unsigned)parts, (unsigned)std::max<int64_t>(1, std::min<int64_t>(n, 32768 / parts)));
-    k_grad_chunk<T, 64, 4, 8><<<g, 256, 0, s>>>(z, ldz, n, classes, q, dz, ldd);
+    k_grad_chunk<T, 64, 4><<<g, 256, 0, s>>>(z, ldz, n, classes, span, q, dz, ldd);
   }
   SSCN_HIP(hipGetLastError());
   return SSCN_OK;

@@ -56,6 +56,27 @@ __device__ __forceinline__ int above_in_row(float of, float v) {
   }
 }
 
+// Of the other 15 lanes of this lane's row that hold this lane's key: the sum
+// of their v, and whether one of them is a lower lane.
+struct Same {
+  float sum;
+  bool before;
+};
+template <int N = 1>
+__device__ __forceinline__ Same same_in_row(int key, float v) {
+  if constexpr (N == 16) {
+    return {0.f, false};
+  } else {
+    constexpr int kRotate = 0x120 + N;
+    const int lane = (int)threadIdx.x & 15;
+    const float other = __uint_as_float(dpp<kRotate>(__float_as_uint(v)));
+    const bool same = (int)dpp<kRotate>((uint32_t)key) == key;
+    const bool lower = (int)dpp<kRotate>((uint32_t)lane) < lane;
+    const Same rest = same_in_row<N + 1>(key, v);
+    return {(same ? other : 0.f) + rest.sum, (same && lower) || rest.before};
+  }
+}
+
 // The largest of the 64-bit keys of L lanes (16 or 64).
 __device__ __forceinline__ uint64_t key_max(uint64_t a, uint32_t lo, uint32_t hi) {
   const uint64_t b = (uint64_t)hi << 32 | lo;
