@@ -16,6 +16,7 @@
 #include "internal.h"
 #include "numeric.h"
 #include "partials.h"
+#include "wave.h"
 
 namespace sscn {
 
@@ -40,57 +41,162 @@ __device__ __forceinline__ float pre_restored(float v, float gamma, float beta) 
 // relu that lets a NaN through.
 __device__ __forceinline__ float relu_nan(float v) { return v <= 0.f ? 0.f : v; }
 
-__device__ __forceinline__ int encode(float d, float v, uint32_t byte, float scale, float gamma, float beta) {
-  if (byte == 255) return 0;
-  const float q = rintf(v * power(254 - byte));
-  const bool want = pre_forward(d, scale, beta) > 0.f;
-  const bool have = pre_restored(q * power(byte), gamma, beta) > 0.f;
-  const int way = gamma > 0.f ? 1 : gamma < 0.f ? -1 : 0;
-  return max(-127, min(127, (int)q + ((int)want - (int)have) * way));
+// How the row-wise kernels below share the work: a thread takes 8 consecutive
+// channels (a piece: 16 or 32 bytes of values, 8 of codes, at whatever alignment
+// the row has; the hardware takes any) of every `rows`-th row, so that the
+// channels' constants stay in its registers; 4 threads make a block of 32
+// channels, 4 blocks() threads a row, and a workgroup of 256 takes several rows
+// at once, or (blockIdx.y) 64 blocks of one.  A row's last piece may be short.
+constexpr int kPiece = 8, kThreads = 256, kSpanBlocks = kThreads / 4;
+struct Place {
+  int col, valid;     // first channel; channels of the piece (0: nothing to do)
+  int block, sub;     // block of the row; piece of the block
+  int64_t row, step;  // first row, and how many on to the next
+};
+__device__ __forceinline__ Place place_of(int c, int blocks) {
+  const int here = min(blocks - (int)blockIdx.y * kSpanBlocks, kSpanBlocks);  // blocks of a row in this workgroup
+  const int lanes = 4 * here, rows = kThreads / lanes;
+  const int in_row = (int)threadIdx.x % lanes, r = (int)threadIdx.x / lanes;
+  Place p;
+  p.block = (int)blockIdx.y * kSpanBlocks + in_row / 4;
+  p.sub = in_row % 4;
+  p.col = p.block * kBlock + p.sub * kPiece;
+  p.valid = max(0, min(kPiece, c - p.col));
+  p.row = r < rows ? (int64_t)blockIdx.x * rows + r : INT64_MAX;  // (threads beyond the last whole row take none)
+  p.step = (int64_t)gridDim.x * rows;
+  return p;
 }
 
-// One half wavefront per block, a lane per channel.
-template <typename T>
-__global__ __launch_bounds__(256) void k_apply_q8(const T* __restrict__ x, int64_t ldx, int64_t n, int c, int blocks,
-                                                  const float* __restrict__ mean, const float* __restrict__ invstd,
-                                                  const float* __restrict__ scale, const float* __restrict__ gamma,
-                                                  const float* __restrict__ beta, T* __restrict__ y, int64_t ldy,
-                                                  int8_t* __restrict__ codes, uint8_t* __restrict__ exponents) {
-  const int lane = threadIdx.x & 31;
-  const int64_t total = n * blocks, step = (int64_t)gridDim.x * 8;
-  // every lane of a wavefront takes part in the maximum: the loop's count is the workgroup's
-  for (int64_t i0 = (int64_t)blockIdx.x * 8; i0 < total; i0 += step) {
-    const int64_t i = i0 + (threadIdx.x >> 5);
-    const int64_t r = i / blocks;
-    const int col = (int)(i - r * blocks) * kBlock + lane;
-    const bool live = i < total && col < c;
-    float d = 0.f, v = 0.f;
-    if (live) {
-      d = ld(x + r * ldx + col) - mean[col];
-      v = d * invstd[col];
-    }
-    uint32_t most = __float_as_uint(v) & 0x7fffffffu;
+// 8 values from / to memory; a short piece value by value.
+__device__ __forceinline__ void load8(const float* p, int valid, float (&x)[kPiece]) {
+  if (valid == kPiece) {
+    __builtin_memcpy(x, p, 32);
+  } else {
 #pragma unroll
-    for (int s = 16; s >= 1; s >>= 1) most = max(most, (uint32_t)__shfl_xor(most, s, 32));
-    const uint32_t byte = exponent_byte(most);
-    if (live) {
-      st(y + r * ldy + col, fmaxf(0.f, pre_forward(d, scale[col], beta[col])));
-      codes[r * c + col] = (int8_t)encode(d, v, byte, scale[col], gamma[col], beta[col]);
-      if (lane == 0) exponents[i] = (uint8_t)byte;
+    for (int i = 0; i < kPiece; ++i) x[i] = i < valid ? p[i] : 0.f;
+  }
+}
+__device__ __forceinline__ void load8(const uint16_t* p, int valid, float (&x)[kPiece]) {
+  if (valid == kPiece) {
+    uint32_t w[4];
+    __builtin_memcpy(w, p, 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) x[i] = i < valid ? ld(p + i) : 0.f;
+  }
+}
+__device__ __forceinline__ void store8(float* p, int valid, const float (&x)[kPiece]) {
+  if (valid == kPiece) {
+    __builtin_memcpy(p, x, 32);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i)
+      if (i < valid) p[i] = x[i];
+  }
+}
+__device__ __forceinline__ void store8(uint16_t* p, int valid, const float (&x)[kPiece]) {
+  if (valid == kPiece) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+    __builtin_memcpy(p, w, 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i)
+      if (i < valid) st(p + i, x[i]);
+  }
+}
+// What 8 codes stand for, u 2^e - 128 2^e of the codes plus 128 (exact, and
+// NaN for the byte 255, whose power is inf).
+__device__ __forceinline__ void decode8(const int8_t* p, int valid, uint32_t byte, float (&v)[kPiece]) {
+  uint32_t w[2] = {0, 0};
+  if (valid == kPiece) {
+    __builtin_memcpy(w, p, 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i)
+      if (i < valid) w[i / 4] |= (uint32_t)(uint8_t)p[i] << 8 * (i % 4);
+  }
+  const float s = power(byte), off = -128.f * s;
+#pragma unroll
+  for (int i = 0; i < kPiece; ++i) v[i] = fmaf((float)((w[i / 4] ^ 0x80808080u) >> 8 * (i % 4) & 0xffu), s, off);
+}
+// Per-channel constants of a piece.
+__device__ __forceinline__ void constants(const float* p, const Place& w, float (&k)[kPiece]) {
+#pragma unroll
+  for (int i = 0; i < kPiece; ++i) k[i] = i < w.valid ? p[w.col + i] : 0.f;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_apply_q8(const T* __restrict__ x, int64_t ldx, int64_t n, int c,
+                                                       int blocks, const float* __restrict__ mean,
+                                                       const float* __restrict__ invstd,
+                                                       const float* __restrict__ scale,
+                                                       const float* __restrict__ gamma,
+                                                       const float* __restrict__ beta, T* __restrict__ y, int64_t ldy,
+                                                       int8_t* __restrict__ codes, uint8_t* __restrict__ exponents) {
+  const Place w = place_of(c, blocks);
+  float mu[kPiece], is[kPiece], sc[kPiece], ga[kPiece], be[kPiece];
+  constants(mean, w, mu);
+  constants(invstd, w, is);
+  constants(scale, w, sc);
+  constants(gamma, w, ga);
+  constants(beta, w, be);
+  // the four threads of a block share its maximum: all of them take every turn
+  for (int64_t r = w.row; r < n; r += w.step) {
+    float d[kPiece], v[kPiece], most = 0.f;
+    load8(x + r * ldx + w.col, w.valid, d);
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) {
+      d[i] -= mu[i];
+      v[i] = d[i] * is[i];
+      most = OpMax::of(most, fabsf(v[i]));  // 0 past the row's end
+    }
+    most = wave_reduce<OpMax, 1, 4>(most);
+    const uint32_t byte = exponent_byte(__float_as_uint(most) & 0x7fffffffu);
+    const float up = power(254 - byte), down = power(byte);
+    float a[kPiece];
+    uint32_t q8[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) {
+      const float pre = pre_forward(d[i], sc[i], be[i]);
+      a[i] = fmaxf(0.f, pre);
+      const float q = rintf(v[i] * up);
+      const bool want = pre > 0.f, have = pre_restored(q * down, ga[i], be[i]) > 0.f;
+      // towards the side of the forward
+      const float way = want == have || ga[i] == 0.f ? 0.f : (ga[i] > 0.f) == want ? 1.f : -1.f;
+      const int code = byte == 255 ? 0 : (int)fminf(fmaxf(q + way, -127.f), 127.f);
+      q8[i / 4] |= (uint32_t)(uint8_t)code << 8 * (i % 4);
+    }
+    store8(y + r * ldy + w.col, w.valid, a);
+    int8_t* to = codes + r * c + w.col;
+    if (w.valid == kPiece) {
+      __builtin_memcpy(to, q8, 8);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i)
+        if (i < w.valid) to[i] = (int8_t)(q8[i / 4] >> 8 * (i % 4));
+    }
+    if (w.sub == 0) exponents[r * blocks + w.block] = (uint8_t)byte;
   }
 }
 
 // The values that the codes stand for.
 template <typename T>
-__global__ __launch_bounds__(256) void k_q8_values(const int8_t* __restrict__ codes,
-                                                   const uint8_t* __restrict__ exponents, int64_t n, int c, int blocks,
-                                                   T* __restrict__ y, int64_t ldy) {
-  const int64_t total = n * c;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / c;
-    const int col = (int)(i - r * c);
-    st(y + r * ldy + col, (float)codes[i] * power(exponents[r * blocks + col / kBlock]));
+__global__ __launch_bounds__(kThreads) void k_q8_values(const int8_t* __restrict__ codes,
+                                                        const uint8_t* __restrict__ exponents, int64_t n, int c,
+                                                        int blocks, T* __restrict__ y, int64_t ldy) {
+  const Place w = place_of(c, blocks);
+  if (w.valid == 0) return;
+  for (int64_t r = w.row; r < n; r += w.step) {
+    float v[kPiece];
+    decode8(codes + r * c + w.col, w.valid, exponents[r * blocks + w.block], v);
+    store8(y + r * ldy + w.col, w.valid, v);
   }
 }
 
@@ -98,37 +204,96 @@ __global__ __launch_bounds__(256) void k_q8_values(const int8_t* __restrict__ co
 // ReLU passes, over the rows of this workgroup (a fixed set, added in a fixed
 // order), and the restored activations.
 template <typename T>
-__global__ __launch_bounds__(256) void k_params_q8(const T* __restrict__ da, int64_t ldd,
-                                                   const int8_t* __restrict__ codes,
-                                                   const uint8_t* __restrict__ exponents, int64_t n, int c, int blocks,
-                                                   const float* __restrict__ gamma, const float* __restrict__ beta,
-                                                   T* __restrict__ a, int64_t lda, double* __restrict__ partial) {
-  __shared__ double red[2][4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int col = blockIdx.y * 64 + lane;
-  double a0 = 0.0, a1 = 0.0;
-  if (col < c) {
-    const float ga = gamma[col], be = beta[col];
-    for (int64_t r = (int64_t)blockIdx.x * 4 + wave; r < n; r += (int64_t)gridDim.x * 4) {
-      const float v = (float)codes[r * c + col] * power(exponents[r * blocks + col / kBlock]);
-      const float pre = pre_restored(v, ga, be);
-      const float dz = pre > 0.f ? ld(da + r * ldd + col) : 0.f;
-      a0 += dz;
-      a1 += (double)dz * (double)v;
-      if (a) st(a + r * lda + col, relu_nan(pre));
+__global__ __launch_bounds__(kThreads) void k_params_q8(const T* __restrict__ da, int64_t ldd,
+                                                        const int8_t* __restrict__ codes,
+                                                        const uint8_t* __restrict__ exponents, int64_t n, int c,
+                                                        int blocks, const float* __restrict__ gamma,
+                                                        const float* __restrict__ beta, T* __restrict__ a, int64_t lda,
+                                                        double* __restrict__ partial) {
+  __shared__ double red[kPiece][kThreads + 1];
+  const Place w = place_of(c, blocks);
+  float ga[kPiece], be[kPiece];
+  constants(gamma, w, ga);
+  constants(beta, w, be);
+  double s0[kPiece], s1[kPiece];
+#pragma unroll
+  for (int i = 0; i < kPiece; ++i) s0[i] = s1[i] = 0.0;
+  if (w.valid > 0)
+    for (int64_t r = w.row; r < n; r += w.step) {
+      float d[kPiece], v[kPiece], out[kPiece];
+      load8(da + r * ldd + w.col, w.valid, d);
+      decode8(codes + r * c + w.col, w.valid, exponents[r * blocks + w.block], v);
+#pragma unroll
+      for (int i = 0; i < kPiece; ++i) {
+        const float pre = pre_restored(v[i], ga[i], be[i]);
+        const float dz = pre > 0.f ? d[i] : 0.f;
+        s0[i] += dz;
+        s1[i] = fma((double)dz, (double)v[i], s1[i]);
+        out[i] = relu_nan(pre);
+      }
+      if (a) store8(a + r * lda + w.col, w.valid, out);
+    }
+  // thread t < 8 lanes adds the workgroup's rows of channel t of its span, in order
+  const int here = min(blocks - (int)blockIdx.y * kSpanBlocks, kSpanBlocks), lanes = 4 * here, rows = kThreads / lanes;
+  const int c0 = (int)blockIdx.y * kSpanBlocks * kBlock;
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) red[i][threadIdx.x] = kind ? s1[i] : s0[i];
+    __syncthreads();
+    for (int t = threadIdx.x; t < min(c - c0, here * kBlock); t += kThreads) {
+      double sum = 0.0;
+      for (int q = 0; q < rows; ++q) sum += red[t % kPiece][q * lanes + t / kPiece];
+      partial[((int64_t)blockIdx.x * 2 + kind) * c + c0 + t] = sum;
     }
   }
-  red[0][wave][lane] = a0;
-  red[1][wave][lane] = a1;
-  __syncthreads();
-  if (wave == 0 && col < c) {
-    partial[((int64_t)blockIdx.x * 2) * c + col] = (red[0][0][lane] + red[0][1][lane]) + (red[0][2][lane] + red[0][3][lane]);
-    partial[((int64_t)blockIdx.x * 2 + 1) * c + col] = (red[1][0][lane] + red[1][1][lane]) + (red[1][2][lane] + red[1][3][lane]);
+}
+
+// dx for the channels [col0, col0 + cols), col0 a multiple of 8 (so that a piece
+// lies in one block).
+template <typename T>
+__global__ __launch_bounds__(kThreads) void k_input_q8_pieces(
+    const T* __restrict__ da, int64_t ldd, const int8_t* __restrict__ codes, const uint8_t* __restrict__ exponents,
+    int64_t n, int c, int blocks, int col0, int cols, const float* __restrict__ gamma, const float* __restrict__ beta,
+    const float* __restrict__ invstd, const float* __restrict__ dgamma, const float* __restrict__ dbeta,
+    const T* __restrict__ add, int64_t lda, T* __restrict__ dx, int64_t ldo) {
+  Place w = place_of(cols, (int)((cols + kBlock - 1) / kBlock));
+  if (w.valid == 0) return;
+  const int k = w.col;  // first channel of the range's own columns
+  w.col += col0;
+  const float inv_n = 1.f / (float)n;
+  float ga[kPiece], be[kPiece], m0[kPiece], m1[kPiece], gi[kPiece];
+  constants(gamma, w, ga);
+  constants(beta, w, be);
+  constants(dbeta, w, m0);
+  constants(dgamma, w, m1);
+  constants(invstd, w, gi);
+#pragma unroll
+  for (int i = 0; i < kPiece; ++i) {
+    m0[i] *= inv_n;
+    m1[i] *= inv_n;
+    gi[i] *= ga[i];
+  }
+  const uint8_t* exps = exponents + w.col / kBlock;
+  for (int64_t r = w.row; r < n; r += w.step) {
+    float d[kPiece], v[kPiece], out[kPiece];
+    load8(da + r * ldd + w.col, w.valid, d);
+    decode8(codes + r * c + w.col, w.valid, exps[r * blocks], v);
+    if (add) load8(add + r * lda + k, w.valid, out);
+#pragma unroll
+    for (int i = 0; i < kPiece; ++i) {
+      const float dz = pre_restored(v[i], ga[i], be[i]) > 0.f ? d[i] : 0.f;
+      const float g = gi[i] * (dz - m0[i] - v[i] * m1[i]);
+      out[i] = add ? g + out[i] : g;
+    }
+    store8(dx + r * ldo + k, w.valid, out);
   }
 }
 
 // dx = gamma invstd (dz - dbeta / n - xhat dgamma / n) (+ add) for the columns
-// [col0, col0 + cols) of the layer; dx and add hold just those.
+// [col0, col0 + cols) of the layer; dx and add hold just those.  An element a
+// lane: for ranges that start inside a piece.
 template <typename T>
 __global__ __launch_bounds__(256) void k_input_q8(const T* __restrict__ da, int64_t ldd,
                                                   const int8_t* __restrict__ codes,
@@ -151,8 +316,14 @@ __global__ __launch_bounds__(256) void k_input_q8(const T* __restrict__ da, int6
   }
 }
 
-int row_blocks(int64_t n) { return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(n, 64), kMaxPartials)); }
 unsigned grid_of(int64_t work) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(work, 16384)); }
+// Grid of the kernels that go by Place, `most` workgroups over the rows at most.
+dim3 place_grid(int64_t n, int blocks, int64_t most) {
+  const int spans = (int)ceil_div(blocks, kSpanBlocks), rows = kThreads / (4 * std::min(blocks, kSpanBlocks));
+  return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(n, rows), most)), (unsigned)spans);
+}
+// Workgroups over the rows of the row-wise kernels: 256 CUs hold some 6 each.
+constexpr int64_t kRowGroups = 2048;
 
 sscn_status check_dtype(sscn_dtype dtype) {
   if (dtype != SSCN_F32 && dtype != SSCN_BF16) return fail(SSCN_ERR_INVALID_ARG, "unknown dtype");
@@ -189,7 +360,7 @@ extern "C" sscn_status sscn_batchnorm_relu_apply_q8(const void* x, int64_t ldx, 
     return fail(SSCN_ERR_INVALID_ARG, "q8: NULL mean, invstd, scale, gamma or beta");
   if (n == 0) return SSCN_OK;
   const int blocks = (int)ceil_div(c, kBlock);
-  const unsigned g = grid_of(ceil_div(n * blocks, 8));
+  const dim3 g = place_grid(n, blocks, kRowGroups);
   if (dtype == SSCN_F32)
     k_apply_q8<float><<<g, 256, 0, stream>>>((const float*)x, ldx, n, c, blocks, mean, invstd, scale, gamma, beta,
                                              (float*)y, ldy, codes, exponents);
@@ -207,7 +378,7 @@ extern "C" sscn_status sscn_q8_values(const int8_t* codes, const uint8_t* expone
   SSCN_TRY(check_codes(codes, exponents, n));
   if (n == 0) return SSCN_OK;
   const int blocks = (int)ceil_div(c, kBlock);
-  const unsigned g = grid_of(ceil_div(n * c, 256));
+  const dim3 g = place_grid(n, blocks, kRowGroups);
   if (dtype == SSCN_F32)
     k_q8_values<float><<<g, 256, 0, stream>>>(codes, exponents, n, c, blocks, (float*)y, ldy);
   else
@@ -219,7 +390,7 @@ extern "C" sscn_status sscn_q8_values(const int8_t* codes, const uint8_t* expone
 extern "C" sscn_status sscn_batchnorm_relu_backward_params_q8_workspace(int64_t n, int32_t c, int64_t* bytes) {
   if (n < 0 || c < 1) return fail(SSCN_ERR_INVALID_ARG, "q8: n must be >= 0 and c >= 1");
   if (!bytes) return fail(SSCN_ERR_INVALID_ARG, "q8: NULL bytes");
-  *bytes = (int64_t)sizeof(double) * 2 * row_blocks(n) * c;
+  *bytes = (int64_t)sizeof(double) * 2 * place_grid(n, (int)ceil_div(c, kBlock), kMaxPartials).x * c;
   return SSCN_OK;
 }
 
@@ -238,8 +409,9 @@ extern "C" sscn_status sscn_batchnorm_relu_backward_params_q8(const void* da, in
   SSCN_TRY(sscn_batchnorm_relu_backward_params_q8_workspace(n, c, &need));
   if (workspace_bytes < need || !workspace || reinterpret_cast<uintptr_t>(workspace) % sizeof(double) != 0)
     return fail(SSCN_ERR_INVALID_ARG, "q8: no workspace of the size that ..._params_q8_workspace says, 8-byte aligned");
-  const int blocks = (int)ceil_div(c, kBlock), parts = row_blocks(n);
-  const dim3 grid((unsigned)parts, (unsigned)ceil_div(c, 64));
+  const int blocks = (int)ceil_div(c, kBlock);
+  const dim3 grid = place_grid(n, blocks, kMaxPartials);
+  const int parts = (int)grid.x;
   double* partial = (double*)workspace;
   if (dtype == SSCN_F32)
     k_params_q8<float><<<grid, 256, 0, stream>>>((const float*)da, ldd, codes, exponents, n, c, blocks, gamma, beta,
@@ -271,6 +443,19 @@ extern "C" sscn_status sscn_batchnorm_relu_backward_input_q8(const void* da, int
     return fail(SSCN_ERR_INVALID_ARG, "q8: NULL parameters or statistics");
   if (n == 0) return SSCN_OK;
   const int blocks = (int)ceil_div(c, kBlock);
+  if (col0 % kPiece == 0) {
+    const dim3 g = place_grid(n, (int)ceil_div(cols, kBlock), kRowGroups);
+    if (dtype == SSCN_F32)
+      k_input_q8_pieces<float><<<g, kThreads, 0, stream>>>((const float*)da, ldd, codes, exponents, n, c, blocks, col0,
+                                                           cols, gamma, beta, invstd, dgamma, dbeta,
+                                                           (const float*)add, ld_add, (float*)dx, ldx_out);
+    else
+      k_input_q8_pieces<uint16_t><<<g, kThreads, 0, stream>>>(
+          (const uint16_t*)da, ldd, codes, exponents, n, c, blocks, col0, cols, gamma, beta, invstd, dgamma, dbeta,
+          (const uint16_t*)add, ld_add, (uint16_t*)dx, ldx_out);
+    SSCN_HIP(hipGetLastError());
+    return SSCN_OK;
+  }
   const unsigned g = grid_of(ceil_div(n * cols, 256));
   if (dtype == SSCN_F32)
     k_input_q8<float><<<g, 256, 0, stream>>>((const float*)da, ldd, codes, exponents, n, c, blocks, col0, cols, gamma,

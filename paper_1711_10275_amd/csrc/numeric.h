@@ -24,4 +24,11 @@ __device__ __forceinline__ float ld(const uint16_t* p) { return bf16_bits_f32(*p
 __device__ __forceinline__ void st(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st(uint16_t* p, float v) { *p = f32_bf16_bits(v); }
 
+// Two bfloat16 in a word, each to nearest, ties to even; NaN stays NaN.
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  typedef __bf16 B2 __attribute__((ext_vector_type(2)));
+  typedef float F2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(F2{lo, hi}, B2));
+}
+
 }  // namespace sscn

@@ -768,12 +768,6 @@ __device__ __forceinline__ float grad_direct(const GradRow& w, float x, float A)
   const float lp = (x - w.base) - w.L, p = expf(lp);
   return -A * expm1f(lp) - p * ((w.G - A) + (p == 0.f ? 0.f : w.h * (lp + w.H)));
 }
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {  // nearest even, NaN kept
-  typedef __bf16 B2 __attribute__((ext_vector_type(2)));
-  typedef float F2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector(F2{lo, hi}, B2));
-}
-
 // Short rows, a thread per row as in k_scores_rows.  The 64 rows of a
 // wavefront go out through LDS, rows an odd number of words apart (each lane
 // its own bank), as consecutive words of 4 bytes (WORDS) or single values.
