@@ -41,43 +41,45 @@ __device__ __forceinline__ float pre_restored(float v, float gamma, float beta) 
 // relu that lets a NaN through.
 __device__ __forceinline__ float relu_nan(float v) { return v <= 0.f ? 0.f : v; }
 
-// How the row-wise kernels below share the work: a thread takes 8 consecutive
-// channels (a piece: 16 or 32 bytes of values, 8 of codes, at whatever alignment
-// the row has; the hardware takes any) of every `rows`-th row, so that the
-// channels' constants stay in its registers; 4 threads make a block of 32
-// channels, 4 blocks() threads a row, and a workgroup of 256 takes several rows
-// at once, or (blockIdx.y) 64 blocks of one.  A row's last piece may be short.
-constexpr int kPiece = 8, kThreads = 256, kSpanBlocks = kThreads / 4;
+// How the row-wise kernels below share the work: a thread takes a piece of P
+// consecutive channels (16 bytes of values, 4 in fp32 and 8 in bf16, at whatever
+// alignment the row has; the hardware takes any) of every so many rows, so that
+// the channels' constants stay in its registers; 32 / P threads make a block of
+// 32 channels, a workgroup of 256 takes several rows at once, or (blockIdx.y)
+// 8 P blocks of one.  A row's last piece may be short.
+constexpr int kThreads = 256;
+template <int P>
 struct Place {
+  static constexpr int kLanes = kBlock / P, kSpan = kThreads / kLanes;  // threads to a block, blocks to a workgroup
   int col, valid;     // first channel; channels of the piece (0: nothing to do)
   int block, sub;     // block of the row; piece of the block
   int64_t row, step;  // first row, and how many on to the next
+  __device__ Place(int c, int blocks) {
+    const int lanes = kLanes * min(blocks - (int)blockIdx.y * kSpan, kSpan), rows = kThreads / lanes;
+    const int in_row = (int)threadIdx.x % lanes, r = (int)threadIdx.x / lanes;
+    block = (int)blockIdx.y * kSpan + in_row / kLanes;
+    sub = in_row % kLanes;
+    col = block * kBlock + sub * P;
+    valid = max(0, min(P, c - col));
+    row = r < rows ? (int64_t)blockIdx.x * rows + r : INT64_MAX;  // (threads beyond the last whole row take none)
+    step = (int64_t)gridDim.x * rows;
+  }
 };
-__device__ __forceinline__ Place place_of(int c, int blocks) {
-  const int here = min(blocks - (int)blockIdx.y * kSpanBlocks, kSpanBlocks);  // blocks of a row in this workgroup
-  const int lanes = 4 * here, rows = kThreads / lanes;
-  const int in_row = (int)threadIdx.x % lanes, r = (int)threadIdx.x / lanes;
-  Place p;
-  p.block = (int)blockIdx.y * kSpanBlocks + in_row / 4;
-  p.sub = in_row % 4;
-  p.col = p.block * kBlock + p.sub * kPiece;
-  p.valid = max(0, min(kPiece, c - p.col));
-  p.row = r < rows ? (int64_t)blockIdx.x * rows + r : INT64_MAX;  // (threads beyond the last whole row take none)
-  p.step = (int64_t)gridDim.x * rows;
-  return p;
-}
+template <typename T>
+constexpr int kPiece = 16 / (int)sizeof(T);
 
-// 8 values from / to memory; a short piece value by value.
-__device__ __forceinline__ void load8(const float* p, int valid, float (&x)[kPiece]) {
-  if (valid == kPiece) {
-    __builtin_memcpy(x, p, 32);
+// A piece from / to memory; a short one value by value.
+template <int P>
+__device__ __forceinline__ void load_piece(const float* p, int valid, float (&x)[P]) {
+  if (valid == P) {
+    __builtin_memcpy(x, p, 4 * P);
   } else {
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i) x[i] = i < valid ? p[i] : 0.f;
+    for (int i = 0; i < P; ++i) x[i] = i < valid ? p[i] : 0.f;
   }
 }
-__device__ __forceinline__ void load8(const uint16_t* p, int valid, float (&x)[kPiece]) {
-  if (valid == kPiece) {
+__device__ __forceinline__ void load_piece(const uint16_t* p, int valid, float (&x)[8]) {
+  if (valid == 8) {
     uint32_t w[4];
     __builtin_memcpy(w, p, 16);
 #pragma unroll
@@ -87,49 +89,45 @@ __device__ __forceinline__ void load8(const uint16_t* p, int valid, float (&x)[k
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i) x[i] = i < valid ? ld(p + i) : 0.f;
+    for (int i = 0; i < 8; ++i) x[i] = i < valid ? ld(p + i) : 0.f;
   }
 }
-__device__ __forceinline__ void store8(float* p, int valid, const float (&x)[kPiece]) {
-  if (valid == kPiece) {
-    __builtin_memcpy(p, x, 32);
+__device__ __forceinline__ void store_piece(float* p, int valid, const float (&x)[4]) {
+  if (valid == 4) {
+    __builtin_memcpy(p, x, 16);
   } else {
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i)
+    for (int i = 0; i < 4; ++i)
       if (i < valid) p[i] = x[i];
   }
 }
-__device__ __forceinline__ void store8(uint16_t* p, int valid, const float (&x)[kPiece]) {
-  if (valid == kPiece) {
+__device__ __forceinline__ void store_piece(uint16_t* p, int valid, const float (&x)[8]) {
+  if (valid == 8) {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
     __builtin_memcpy(p, w, 16);
   } else {
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i)
+    for (int i = 0; i < 8; ++i)
       if (i < valid) st(p + i, x[i]);
   }
 }
-// What 8 codes stand for, u 2^e - 128 2^e of the codes plus 128 (exact, and
-// NaN for the byte 255, whose power is inf).
-__device__ __forceinline__ void decode8(const int8_t* p, int valid, uint32_t byte, float (&v)[kPiece]) {
-  uint32_t w[2] = {0, 0};
-  if (valid == kPiece) {
-    __builtin_memcpy(w, p, 8);
+// What a piece's codes stand for, u 2^e - 128 2^e of the codes plus 128 (exact,
+// and NaN for the byte 255, whose power is inf).
+template <int P>
+__device__ __forceinline__ void decode_piece(const int8_t* p, int valid, uint32_t byte, float (&v)[P]) {
+  uint32_t w[P / 4] = {};
+  if (valid == P) {
+    __builtin_memcpy(w, p, P);
   } else {
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i)
+    for (int i = 0; i < P; ++i)
       if (i < valid) w[i / 4] |= (uint32_t)(uint8_t)p[i] << 8 * (i % 4);
   }
   const float s = power(byte), off = -128.f * s;
 #pragma unroll
-  for (int i = 0; i < kPiece; ++i) v[i] = fmaf((float)((w[i / 4] ^ 0x80808080u) >> 8 * (i % 4) & 0xffu), s, off);
-}
-// Per-channel constants of a piece.
-__device__ __forceinline__ void constants(const float* p, const Place& w, float (&k)[kPiece]) {
-#pragma unroll
-  for (int i = 0; i < kPiece; ++i) k[i] = i < w.valid ? p[w.col + i] : 0.f;
+  for (int i = 0; i < P; ++i) v[i] = fmaf((float)((w[i / 4] ^ 0x80808080u) >> 8 * (i % 4) & 0xffu), s, off);
 }
 
 template <typename T>
@@ -140,30 +138,31 @@ __global__ __launch_bounds__(kThreads) void k_apply_q8(const T* __restrict__ x, 
                                                        const float* __restrict__ gamma,
                                                        const float* __restrict__ beta, T* __restrict__ y, int64_t ldy,
                                                        int8_t* __restrict__ codes, uint8_t* __restrict__ exponents) {
-  const Place w = place_of(c, blocks);
-  float mu[kPiece], is[kPiece], sc[kPiece], ga[kPiece], be[kPiece];
-  constants(mean, w, mu);
-  constants(invstd, w, is);
-  constants(scale, w, sc);
-  constants(gamma, w, ga);
-  constants(beta, w, be);
-  // the four threads of a block share its maximum: all of them take every turn
+  constexpr int P = kPiece<T>;
+  const Place<P> w(c, blocks);
+  float mu[P], is[P], sc[P], ga[P], be[P];
+  load_piece<P>(mean + w.col, w.valid, mu);
+  load_piece<P>(invstd + w.col, w.valid, is);
+  load_piece<P>(scale + w.col, w.valid, sc);
+  load_piece<P>(gamma + w.col, w.valid, ga);
+  load_piece<P>(beta + w.col, w.valid, be);
+  // the threads of a block share its maximum: all of them take every turn
   for (int64_t r = w.row; r < n; r += w.step) {
-    float d[kPiece], v[kPiece], most = 0.f;
-    load8(x + r * ldx + w.col, w.valid, d);
+    float d[P], v[P], most = 0.f;
+    load_piece(x + r * ldx + w.col, w.valid, d);
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i) {
+    for (int i = 0; i < P; ++i) {
       d[i] -= mu[i];
       v[i] = d[i] * is[i];
       most = OpMax::of(most, fabsf(v[i]));  // 0 past the row's end
     }
-    most = wave_reduce<OpMax, 1, 4>(most);
+    most = wave_reduce<OpMax, 1, Place<P>::kLanes>(most);
     const uint32_t byte = exponent_byte(__float_as_uint(most) & 0x7fffffffu);
     const float up = power(254 - byte), down = power(byte);
-    float a[kPiece];
-    uint32_t q8[2] = {0, 0};
+    float a[P];
+    uint32_t q8[P / 4] = {};
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i) {
+    for (int i = 0; i < P; ++i) {
       const float pre = pre_forward(d[i], sc[i], be[i]);
       a[i] = fmaxf(0.f, pre);
       const float q = rintf(v[i] * up);
@@ -173,13 +172,13 @@ __global__ __launch_bounds__(kThreads) void k_apply_q8(const T* __restrict__ x, 
       const int code = byte == 255 ? 0 : (int)fminf(fmaxf(q + way, -127.f), 127.f);
       q8[i / 4] |= (uint32_t)(uint8_t)code << 8 * (i % 4);
     }
-    store8(y + r * ldy + w.col, w.valid, a);
+    store_piece(y + r * ldy + w.col, w.valid, a);
     int8_t* to = codes + r * c + w.col;
-    if (w.valid == kPiece) {
-      __builtin_memcpy(to, q8, 8);
+    if (w.valid == P) {
+      __builtin_memcpy(to, q8, P);
     } else {
 #pragma unroll
-      for (int i = 0; i < kPiece; ++i)
+      for (int i = 0; i < P; ++i)
         if (i < w.valid) to[i] = (int8_t)(q8[i / 4] >> 8 * (i % 4));
     }
     if (w.sub == 0) exponents[r * blocks + w.block] = (uint8_t)byte;
@@ -191,12 +190,13 @@ template <typename T>
 __global__ __launch_bounds__(kThreads) void k_q8_values(const int8_t* __restrict__ codes,
                                                         const uint8_t* __restrict__ exponents, int64_t n, int c,
                                                         int blocks, T* __restrict__ y, int64_t ldy) {
-  const Place w = place_of(c, blocks);
+  constexpr int P = kPiece<T>;
+  const Place<P> w(c, blocks);
   if (w.valid == 0) return;
   for (int64_t r = w.row; r < n; r += w.step) {
-    float v[kPiece];
-    decode8(codes + r * c + w.col, w.valid, exponents[r * blocks + w.block], v);
-    store8(y + r * ldy + w.col, w.valid, v);
+    float v[P];
+    decode_piece(codes + r * c + w.col, w.valid, exponents[r * blocks + w.block], v);
+    store_piece(y + r * ldy + w.col, w.valid, v);
   }
 }
 
@@ -210,84 +210,87 @@ __global__ __launch_bounds__(kThreads) void k_params_q8(const T* __restrict__ da
                                                         int blocks, const float* __restrict__ gamma,
                                                         const float* __restrict__ beta, T* __restrict__ a, int64_t lda,
                                                         double* __restrict__ partial) {
-  __shared__ double red[kPiece][kThreads + 1];
-  const Place w = place_of(c, blocks);
-  float ga[kPiece], be[kPiece];
-  constants(gamma, w, ga);
-  constants(beta, w, be);
-  double s0[kPiece], s1[kPiece];
+  constexpr int P = kPiece<T>;
+  __shared__ double red[P][kThreads + 1];
+  const Place<P> w(c, blocks);
+  float ga[P], be[P];
+  load_piece<P>(gamma + w.col, w.valid, ga);
+  load_piece<P>(beta + w.col, w.valid, be);
+  double s0[P], s1[P];
 #pragma unroll
-  for (int i = 0; i < kPiece; ++i) s0[i] = s1[i] = 0.0;
+  for (int i = 0; i < P; ++i) s0[i] = s1[i] = 0.0;
   if (w.valid > 0)
     for (int64_t r = w.row; r < n; r += w.step) {
-      float d[kPiece], v[kPiece], out[kPiece];
-      load8(da + r * ldd + w.col, w.valid, d);
-      decode8(codes + r * c + w.col, w.valid, exponents[r * blocks + w.block], v);
+      float d[P], v[P], out[P];
+      load_piece(da + r * ldd + w.col, w.valid, d);
+      decode_piece(codes + r * c + w.col, w.valid, exponents[r * blocks + w.block], v);
 #pragma unroll
-      for (int i = 0; i < kPiece; ++i) {
+      for (int i = 0; i < P; ++i) {
         const float pre = pre_restored(v[i], ga[i], be[i]);
         const float dz = pre > 0.f ? d[i] : 0.f;
         s0[i] += dz;
         s1[i] = fma((double)dz, (double)v[i], s1[i]);
         out[i] = relu_nan(pre);
       }
-      if (a) store8(a + r * lda + w.col, w.valid, out);
+      if (a) store_piece(a + r * lda + w.col, w.valid, out);
     }
-  // thread t < 8 lanes adds the workgroup's rows of channel t of its span, in order
-  const int here = min(blocks - (int)blockIdx.y * kSpanBlocks, kSpanBlocks), lanes = 4 * here, rows = kThreads / lanes;
-  const int c0 = (int)blockIdx.y * kSpanBlocks * kBlock;
+  // thread t adds the workgroup's rows of channel t of its span, in order
+  constexpr int kSpan = Place<P>::kSpan;
+  const int here = min(blocks - (int)blockIdx.y * kSpan, kSpan), lanes = Place<P>::kLanes * here;
+  const int rows = kThreads / lanes, c0 = (int)blockIdx.y * kSpan * kBlock;
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i) red[i][threadIdx.x] = kind ? s1[i] : s0[i];
+    for (int i = 0; i < P; ++i) red[i][threadIdx.x] = kind ? s1[i] : s0[i];
     __syncthreads();
     for (int t = threadIdx.x; t < min(c - c0, here * kBlock); t += kThreads) {
       double sum = 0.0;
-      for (int q = 0; q < rows; ++q) sum += red[t % kPiece][q * lanes + t / kPiece];
+      for (int q = 0; q < rows; ++q) sum += red[t % P][q * lanes + t / P];
       partial[((int64_t)blockIdx.x * 2 + kind) * c + c0 + t] = sum;
     }
   }
 }
 
-// dx for the channels [col0, col0 + cols), col0 a multiple of 8 (so that a piece
-// lies in one block).
+// dx for the channels [col0, col0 + cols), col0 a multiple of the piece (so that
+// one lies in one block).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_input_q8_pieces(
     const T* __restrict__ da, int64_t ldd, const int8_t* __restrict__ codes, const uint8_t* __restrict__ exponents,
     int64_t n, int c, int blocks, int col0, int cols, const float* __restrict__ gamma, const float* __restrict__ beta,
     const float* __restrict__ invstd, const float* __restrict__ dgamma, const float* __restrict__ dbeta,
     const T* __restrict__ add, int64_t lda, T* __restrict__ dx, int64_t ldo) {
-  Place w = place_of(cols, (int)((cols + kBlock - 1) / kBlock));
+  constexpr int P = kPiece<T>;
+  Place<P> w(cols, (cols + kBlock - 1) / kBlock);
   if (w.valid == 0) return;
   const int k = w.col;  // first channel of the range's own columns
   w.col += col0;
   const float inv_n = 1.f / (float)n;
-  float ga[kPiece], be[kPiece], m0[kPiece], m1[kPiece], gi[kPiece];
-  constants(gamma, w, ga);
-  constants(beta, w, be);
-  constants(dbeta, w, m0);
-  constants(dgamma, w, m1);
-  constants(invstd, w, gi);
+  float ga[P], be[P], m0[P], m1[P], gi[P];
+  load_piece<P>(gamma + w.col, w.valid, ga);
+  load_piece<P>(beta + w.col, w.valid, be);
+  load_piece<P>(dbeta + w.col, w.valid, m0);
+  load_piece<P>(dgamma + w.col, w.valid, m1);
+  load_piece<P>(invstd + w.col, w.valid, gi);
 #pragma unroll
-  for (int i = 0; i < kPiece; ++i) {
+  for (int i = 0; i < P; ++i) {
     m0[i] *= inv_n;
     m1[i] *= inv_n;
     gi[i] *= ga[i];
   }
   const uint8_t* exps = exponents + w.col / kBlock;
   for (int64_t r = w.row; r < n; r += w.step) {
-    float d[kPiece], v[kPiece], out[kPiece];
-    load8(da + r * ldd + w.col, w.valid, d);
-    decode8(codes + r * c + w.col, w.valid, exps[r * blocks], v);
-    if (add) load8(add + r * lda + k, w.valid, out);
+    float d[P], v[P], out[P];
+    load_piece(da + r * ldd + w.col, w.valid, d);
+    decode_piece(codes + r * c + w.col, w.valid, exps[r * blocks], v);
+    if (add) load_piece(add + r * lda + k, w.valid, out);
 #pragma unroll
-    for (int i = 0; i < kPiece; ++i) {
+    for (int i = 0; i < P; ++i) {
       const float dz = pre_restored(v[i], ga[i], be[i]) > 0.f ? d[i] : 0.f;
       const float g = gi[i] * (dz - m0[i] - v[i] * m1[i]);
       out[i] = add ? g + out[i] : g;
     }
-    store8(dx + r * ldo + k, w.valid, out);
+    store_piece(dx + r * ldo + k, w.valid, out);
   }
 }
 
@@ -317,10 +320,13 @@ __global__ __launch_bounds__(256) void k_input_q8(const T* __restrict__ da, int6
 }
 
 unsigned grid_of(int64_t work) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(work, 16384)); }
+int piece_of(sscn_dtype dtype) { return dtype == SSCN_F32 ? kPiece<float> : kPiece<uint16_t>; }
 // Grid of the kernels that go by Place, `most` workgroups over the rows at most.
-dim3 place_grid(int64_t n, int blocks, int64_t most) {
-  const int spans = (int)ceil_div(blocks, kSpanBlocks), rows = kThreads / (4 * std::min(blocks, kSpanBlocks));
-  return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(n, rows), most)), (unsigned)spans);
+dim3 place_grid(int64_t n, int blocks, int64_t most, sscn_dtype dtype) {
+  const int lanes = kBlock / piece_of(dtype), span = kThreads / lanes;
+  const int rows = kThreads / (lanes * std::min(blocks, span));
+  return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(n, rows), most)),
+              (unsigned)ceil_div(blocks, span));
 }
 // Workgroups over the rows of the row-wise kernels: 256 CUs hold some 6 each.
 constexpr int64_t kRowGroups = 2048;
@@ -360,7 +366,7 @@ extern "C" sscn_status sscn_batchnorm_relu_apply_q8(const void* x, int64_t ldx, 
     return fail(SSCN_ERR_INVALID_ARG, "q8: NULL mean, invstd, scale, gamma or beta");
   if (n == 0) return SSCN_OK;
   const int blocks = (int)ceil_div(c, kBlock);
-  const dim3 g = place_grid(n, blocks, kRowGroups);
+  const dim3 g = place_grid(n, blocks, kRowGroups, dtype);
   if (dtype == SSCN_F32)
     k_apply_q8<float><<<g, 256, 0, stream>>>((const float*)x, ldx, n, c, blocks, mean, invstd, scale, gamma, beta,
                                              (float*)y, ldy, codes, exponents);
@@ -378,7 +384,7 @@ extern "C" sscn_status sscn_q8_values(const int8_t* codes, const uint8_t* expone
   SSCN_TRY(check_codes(codes, exponents, n));
   if (n == 0) return SSCN_OK;
   const int blocks = (int)ceil_div(c, kBlock);
-  const dim3 g = place_grid(n, blocks, kRowGroups);
+  const dim3 g = place_grid(n, blocks, kRowGroups, dtype);
   if (dtype == SSCN_F32)
     k_q8_values<float><<<g, 256, 0, stream>>>(codes, exponents, n, c, blocks, (float*)y, ldy);
   else
@@ -390,7 +396,8 @@ extern "C" sscn_status sscn_q8_values(const int8_t* codes, const uint8_t* expone
 extern "C" sscn_status sscn_batchnorm_relu_backward_params_q8_workspace(int64_t n, int32_t c, int64_t* bytes) {
   if (n < 0 || c < 1) return fail(SSCN_ERR_INVALID_ARG, "q8: n must be >= 0 and c >= 1");
   if (!bytes) return fail(SSCN_ERR_INVALID_ARG, "q8: NULL bytes");
-  *bytes = (int64_t)sizeof(double) * 2 * place_grid(n, (int)ceil_div(c, kBlock), kMaxPartials).x * c;
+  // (as many workgroups at least as either type's pieces give)
+  *bytes = (int64_t)sizeof(double) * 2 * place_grid(n, (int)ceil_div(c, kBlock), kMaxPartials, SSCN_F32).x * c;
   return SSCN_OK;
 }
 
@@ -410,7 +417,7 @@ extern "C" sscn_status sscn_batchnorm_relu_backward_params_q8(const void* da, in
   if (workspace_bytes < need || !workspace || reinterpret_cast<uintptr_t>(workspace) % sizeof(double) != 0)
     return fail(SSCN_ERR_INVALID_ARG, "q8: no workspace of the size that ..._params_q8_workspace says, 8-byte aligned");
   const int blocks = (int)ceil_div(c, kBlock);
-  const dim3 grid = place_grid(n, blocks, kMaxPartials);
+  const dim3 grid = place_grid(n, blocks, kMaxPartials, dtype);
   const int parts = (int)grid.x;
   double* partial = (double*)workspace;
   if (dtype == SSCN_F32)
@@ -443,8 +450,8 @@ extern "C" sscn_status sscn_batchnorm_relu_backward_input_q8(const void* da, int
     return fail(SSCN_ERR_INVALID_ARG, "q8: NULL parameters or statistics");
   if (n == 0) return SSCN_OK;
   const int blocks = (int)ceil_div(c, kBlock);
-  if (col0 % kPiece == 0) {
-    const dim3 g = place_grid(n, (int)ceil_div(cols, kBlock), kRowGroups);
+  if (col0 % piece_of(dtype) == 0) {
+    const dim3 g = place_grid(n, (int)ceil_div(cols, kBlock), kRowGroups, dtype);
     if (dtype == SSCN_F32)
       k_input_q8_pieces<float><<<g, kThreads, 0, stream>>>((const float*)da, ldd, codes, exponents, n, c, blocks, col0,
                                                            cols, gamma, beta, invstd, dgamma, dbeta,
