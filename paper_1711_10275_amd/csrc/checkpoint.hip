@@ -12,10 +12,10 @@
 // the backward pass masks exactly what the forward masked.  A block that holds
 // an infinity or a NaN has the byte 255 and codes 0: 0 * inf, it stands for NaN.
 #include <algorithm>
+#include <type_traits>
 
 #include "internal.h"
 #include "numeric.h"
-#include "partials.h"
 #include "wave.h"
 
 namespace sscn {
@@ -68,69 +68,87 @@ struct Place {
 template <typename T>
 constexpr int kPiece = 16 / (int)sizeof(T);
 
-// A piece from / to memory; a short one value by value.
-template <int P>
-__device__ __forceinline__ void load_piece(const float* p, int valid, float (&x)[P]) {
+// A piece from memory, as it is stored; a short one (only where CUT says that
+// there may be some) value by value.  Values past the row's end are 0.
+template <typename T, bool CUT>
+__device__ __forceinline__ void load_piece(const T* p, int valid, uint32_t (&w)[4]) {
+  constexpr int P = kPiece<T>;
   if (valid == P) {
-    __builtin_memcpy(x, p, 4 * P);
-  } else {
-#pragma unroll
-    for (int i = 0; i < P; ++i) x[i] = i < valid ? p[i] : 0.f;
-  }
-}
-__device__ __forceinline__ void load_piece(const uint16_t* p, int valid, float (&x)[8]) {
-  if (valid == 8) {
-    uint32_t w[4];
     __builtin_memcpy(w, p, 16);
+  } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(w[i] << 16);
-      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    for (int i = 0; i < 4; ++i) w[i] = 0;
+    if constexpr (CUT) {
+#pragma unroll
+      for (int i = 0; i < P - 1; ++i)
+        if (i < valid) {
+          if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(p[i]);
+          else w[i / 2] |= (uint32_t)p[i] << 16 * (i % 2);
+        }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = i < valid ? ld(p + i) : 0.f;
   }
 }
-__device__ __forceinline__ void store_piece(float* p, int valid, const float (&x)[4]) {
-  if (valid == 4) {
-    __builtin_memcpy(p, x, 16);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (i < valid) p[i] = x[i];
-  }
+template <int P>
+__device__ __forceinline__ float value(const uint32_t (&w)[4], int i) {
+  if constexpr (P == 4) return __uint_as_float(w[i]);
+  else return __uint_as_float(i % 2 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
 }
-__device__ __forceinline__ void store_piece(uint16_t* p, int valid, const float (&x)[8]) {
-  if (valid == 8) {
-    uint32_t w[4];
+template <typename T, bool CUT>
+__device__ __forceinline__ void store_piece(T* p, int valid, const float (&x)[kPiece<T>]) {
+  constexpr int P = kPiece<T>;
+  if (valid == P) {
+    if constexpr (sizeof(T) == 4) {
+      __builtin_memcpy(p, x, 16);
+    } else {
+      uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-    __builtin_memcpy(p, w, 16);
-  } else {
+      for (int i = 0; i < 4; ++i) w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+      __builtin_memcpy(p, w, 16);
+    }
+  } else if constexpr (CUT) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int i = 0; i < P - 1; ++i)
       if (i < valid) st(p + i, x[i]);
   }
 }
-// What a piece's codes stand for, u 2^e - 128 2^e of the codes plus 128 (exact,
-// and NaN for the byte 255, whose power is inf).
-template <int P>
-__device__ __forceinline__ void decode_piece(const int8_t* p, int valid, uint32_t byte, float (&v)[P]) {
-  uint32_t w[P / 4] = {};
+// A piece's codes, and what they stand for: u 2^e - 128 2^e of the codes plus
+// 128 (exact, and NaN for the byte 255, whose power is inf).
+template <int P, bool CUT>
+__device__ __forceinline__ void load_codes(const int8_t* p, int valid, uint32_t (&w)[P / 4]) {
   if (valid == P) {
     __builtin_memcpy(w, p, P);
   } else {
 #pragma unroll
-    for (int i = 0; i < P; ++i)
-      if (i < valid) w[i / 4] |= (uint32_t)(uint8_t)p[i] << 8 * (i % 4);
+    for (int i = 0; i < P / 4; ++i) w[i] = 0;
+    if constexpr (CUT) {
+#pragma unroll
+      for (int i = 0; i < P - 1; ++i)
+        if (i < valid) w[i / 4] |= (uint32_t)(uint8_t)p[i] << 8 * (i % 4);
+    }
   }
+}
+template <int P>
+__device__ __forceinline__ void decode(const uint32_t (&w)[P / 4], uint32_t byte, float (&v)[P]) {
   const float s = power(byte), off = -128.f * s;
 #pragma unroll
   for (int i = 0; i < P; ++i) v[i] = fmaf((float)((w[i / 4] ^ 0x80808080u) >> 8 * (i % 4) & 0xffu), s, off);
 }
+// Per-channel constants of a piece.
+template <int P>
+__device__ __forceinline__ void constants(const float* p, int valid, float (&k)[P]) {
+  if (valid == P) {
+    __builtin_memcpy(k, p, 4 * P);
+  } else {
+#pragma unroll
+    for (int i = 0; i < P; ++i) k[i] = i < valid ? p[i] : 0.f;
+  }
+}
 
-template <typename T>
+// Every kernel takes kRows of its rows a turn, so that their loads are in
+// flight together.
+constexpr int kRows = 2;
+
+template <typename T, bool CUT>
 __global__ __launch_bounds__(kThreads) void k_apply_q8(const T* __restrict__ x, int64_t ldx, int64_t n, int c,
                                                        int blocks, const float* __restrict__ mean,
                                                        const float* __restrict__ invstd,
@@ -141,69 +159,102 @@ __global__ __launch_bounds__(kThreads) void k_apply_q8(const T* __restrict__ x, 
   constexpr int P = kPiece<T>;
   const Place<P> w(c, blocks);
   float mu[P], is[P], sc[P], ga[P], be[P];
-  load_piece<P>(mean + w.col, w.valid, mu);
-  load_piece<P>(invstd + w.col, w.valid, is);
-  load_piece<P>(scale + w.col, w.valid, sc);
-  load_piece<P>(gamma + w.col, w.valid, ga);
-  load_piece<P>(beta + w.col, w.valid, be);
+  constants<P>(mean + w.col, w.valid, mu);
+  constants<P>(invstd + w.col, w.valid, is);
+  constants<P>(scale + w.col, w.valid, sc);
+  constants<P>(gamma + w.col, w.valid, ga);
+  constants<P>(beta + w.col, w.valid, be);
   // the threads of a block share its maximum: all of them take every turn
-  for (int64_t r = w.row; r < n; r += w.step) {
-    float d[P], v[P], most = 0.f;
-    load_piece(x + r * ldx + w.col, w.valid, d);
+  for (int64_t r0 = w.row; r0 < n; r0 += kRows * w.step) {
+    uint32_t in[kRows][4];
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      d[i] -= mu[i];
-      v[i] = d[i] * is[i];
-      most = OpMax::of(most, fabsf(v[i]));  // 0 past the row's end
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t r = r0 + u * w.step;
+      load_piece<T, CUT>(x + r * ldx + w.col, r < n ? w.valid : 0, in[u]);
     }
-    most = wave_reduce<OpMax, 1, Place<P>::kLanes>(most);
-    const uint32_t byte = exponent_byte(__float_as_uint(most) & 0x7fffffffu);
-    const float up = power(254 - byte), down = power(byte);
-    float a[P];
-    uint32_t q8[P / 4] = {};
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const float pre = pre_forward(d[i], sc[i], be[i]);
-      a[i] = fmaxf(0.f, pre);
-      const float q = rintf(v[i] * up);
-      const bool want = pre > 0.f, have = pre_restored(q * down, ga[i], be[i]) > 0.f;
-      // towards the side of the forward
-      const float way = want == have || ga[i] == 0.f ? 0.f : (ga[i] > 0.f) == want ? 1.f : -1.f;
-      const int code = byte == 255 ? 0 : (int)fminf(fmaxf(q + way, -127.f), 127.f);
-      q8[i / 4] |= (uint32_t)(uint8_t)code << 8 * (i % 4);
-    }
-    store_piece(y + r * ldy + w.col, w.valid, a);
-    int8_t* to = codes + r * c + w.col;
-    if (w.valid == P) {
-      __builtin_memcpy(to, q8, P);
-    } else {
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t r = r0 + u * w.step;
+      if (r >= n) break;
+      float d[P], v[P], a[P], most = 0.f;
 #pragma unroll
-      for (int i = 0; i < P; ++i)
-        if (i < w.valid) to[i] = (int8_t)(q8[i / 4] >> 8 * (i % 4));
+      for (int i = 0; i < P; ++i) {
+        d[i] = value<P>(in[u], i) - mu[i];
+        v[i] = d[i] * is[i];
+        most = OpMax::of(most, fabsf(v[i]));  // 0 past the row's end
+      }
+      most = wave_reduce<OpMax, 1, Place<P>::kLanes>(most);
+      const uint32_t byte = exponent_byte(__float_as_uint(most) & 0x7fffffffu);
+      const float up = power(254 - byte), down = power(byte);
+      uint32_t q8[P / 4] = {};
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const float pre = pre_forward(d[i], sc[i], be[i]);
+        a[i] = fmaxf(0.f, pre);
+        const float q = rintf(v[i] * up);
+        const bool want = pre > 0.f, have = pre_restored(q * down, ga[i], be[i]) > 0.f;
+        // towards the side of the forward
+        const float way = want == have || ga[i] == 0.f ? 0.f : (ga[i] > 0.f) == want ? 1.f : -1.f;
+        const int code = byte == 255 ? 0 : (int)fminf(fmaxf(q + way, -127.f), 127.f);
+        q8[i / 4] |= (uint32_t)(uint8_t)code << 8 * (i % 4);
+      }
+      store_piece<T, CUT>(y + r * ldy + w.col, w.valid, a);
+      int8_t* to = codes + r * c + w.col;
+      if (w.valid == P) {
+        __builtin_memcpy(to, q8, P);
+      } else if constexpr (CUT) {
+#pragma unroll
+        for (int i = 0; i < P - 1; ++i)
+          if (i < w.valid) to[i] = (int8_t)(q8[i / 4] >> 8 * (i % 4));
+      }
+      if (w.sub == 0) exponents[r * blocks + w.block] = (uint8_t)byte;
     }
-    if (w.sub == 0) exponents[r * blocks + w.block] = (uint8_t)byte;
   }
 }
 
+// The codes and exponent bytes of kRows rows, and the matrix piece of each.
+template <typename T, bool CUT>
+struct Turn {
+  static constexpr int P = kPiece<T>;
+  uint32_t q[kRows][P / 4], d[kRows][4], byte[kRows];
+  __device__ __forceinline__ Turn(const Place<P>& w, int64_t r0, int64_t n, const int8_t* codes, int c,
+                                  const uint8_t* exps, int blocks, const T* m, int64_t ldm) {
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t r = r0 + u * w.step;
+      const int valid = r < n ? w.valid : 0;
+      if (m) load_piece<T, CUT>(m + r * ldm, valid, d[u]);
+      load_codes<P, CUT>(codes + r * c, valid, q[u]);
+      byte[u] = r < n ? exps[r * blocks] : 0;
+    }
+  }
+};
+
 // The values that the codes stand for.
-template <typename T>
+template <typename T, bool CUT>
 __global__ __launch_bounds__(kThreads) void k_q8_values(const int8_t* __restrict__ codes,
                                                         const uint8_t* __restrict__ exponents, int64_t n, int c,
                                                         int blocks, T* __restrict__ y, int64_t ldy) {
   constexpr int P = kPiece<T>;
   const Place<P> w(c, blocks);
   if (w.valid == 0) return;
-  for (int64_t r = w.row; r < n; r += w.step) {
-    float v[P];
-    decode_piece(codes + r * c + w.col, w.valid, exponents[r * blocks + w.block], v);
-    store_piece(y + r * ldy + w.col, w.valid, v);
+  for (int64_t r0 = w.row; r0 < n; r0 += kRows * w.step) {
+    const Turn<T, CUT> t(w, r0, n, codes + w.col, c, exponents + w.block, blocks, nullptr, 0);
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t r = r0 + u * w.step;
+      if (r >= n) break;
+      float v[P];
+      decode<P>(t.q[u], t.byte[u], v);
+      store_piece<T, CUT>(y + r * ldy + w.col, w.valid, v);
+    }
   }
 }
 
 // Per channel the fp64 sums of dz and dz * xhat, dz = dA where the restored
 // ReLU passes, over the rows of this workgroup (a fixed set, added in a fixed
 // order), and the restored activations.
-template <typename T>
+template <typename T, bool CUT>
 __global__ __launch_bounds__(kThreads) void k_params_q8(const T* __restrict__ da, int64_t ldd,
                                                         const int8_t* __restrict__ codes,
                                                         const uint8_t* __restrict__ exponents, int64_t n, int c,
@@ -214,25 +265,30 @@ __global__ __launch_bounds__(kThreads) void k_params_q8(const T* __restrict__ da
   __shared__ double red[P][kThreads + 1];
   const Place<P> w(c, blocks);
   float ga[P], be[P];
-  load_piece<P>(gamma + w.col, w.valid, ga);
-  load_piece<P>(beta + w.col, w.valid, be);
+  constants<P>(gamma + w.col, w.valid, ga);
+  constants<P>(beta + w.col, w.valid, be);
   double s0[P], s1[P];
 #pragma unroll
   for (int i = 0; i < P; ++i) s0[i] = s1[i] = 0.0;
   if (w.valid > 0)
-    for (int64_t r = w.row; r < n; r += w.step) {
-      float d[P], v[P], out[P];
-      load_piece(da + r * ldd + w.col, w.valid, d);
-      decode_piece(codes + r * c + w.col, w.valid, exponents[r * blocks + w.block], v);
+    for (int64_t r0 = w.row; r0 < n; r0 += kRows * w.step) {
+      const Turn<T, CUT> t(w, r0, n, codes + w.col, c, exponents + w.block, blocks, da + w.col, ldd);
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        const float pre = pre_restored(v[i], ga[i], be[i]);
-        const float dz = pre > 0.f ? d[i] : 0.f;
-        s0[i] += dz;
-        s1[i] = fma((double)dz, (double)v[i], s1[i]);
-        out[i] = relu_nan(pre);
+      for (int u = 0; u < kRows; ++u) {
+        const int64_t r = r0 + u * w.step;
+        if (r >= n) break;
+        float v[P], out[P];
+        decode<P>(t.q[u], t.byte[u], v);
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          const float pre = pre_restored(v[i], ga[i], be[i]);
+          const float dz = pre > 0.f ? value<P>(t.d[u], i) : 0.f;
+          s0[i] += dz;
+          s1[i] = fma((double)dz, (double)v[i], s1[i]);
+          out[i] = relu_nan(pre);
+        }
+        if (a) store_piece<T, CUT>(a + r * lda + w.col, w.valid, out);
       }
-      if (a) store_piece(a + r * lda + w.col, w.valid, out);
     }
   // thread t adds the workgroup's rows of channel t of its span, in order
   constexpr int kSpan = Place<P>::kSpan;
@@ -252,45 +308,88 @@ __global__ __launch_bounds__(kThreads) void k_params_q8(const T* __restrict__ da
   }
 }
 
+// Adds the parts, 16 channels to a workgroup: thread t the parts t / 16, + 64,
+// .. of channel t % 16 in order, then the 64 threads of a channel in a fixed
+// tree.  (64 channels to a workgroup left most CUs without one and took 20 us
+// for 1024 parts of 512 channels.)
+__global__ __launch_bounds__(1024) void k_sum_parts(const double* __restrict__ partial, int parts, int c,
+                                                    float* __restrict__ dbeta, float* __restrict__ dgamma) {
+  __shared__ double red[2][64][16];
+  const int k = threadIdx.x % 16, p0 = threadIdx.x / 16, col = blockIdx.x * 16 + k;
+  double s0 = 0.0, s1 = 0.0;
+  if (col < c) {
+#pragma unroll 4
+    for (int p = p0; p < parts; p += 64) {
+      s0 += partial[((int64_t)p * 2) * c + col];
+      s1 += partial[((int64_t)p * 2 + 1) * c + col];
+    }
+  }
+  red[0][p0][k] = s0;
+  red[1][p0][k] = s1;
+  __syncthreads();
+#pragma unroll
+  for (int h = 32; h >= 1; h /= 2) {
+    if (p0 < h) {
+      red[0][p0][k] += red[0][p0 + h][k];
+      red[1][p0][k] += red[1][p0 + h][k];
+    }
+    __syncthreads();
+  }
+  if (p0 == 0 && col < c) {
+    dbeta[col] = (float)red[0][0][k];
+    dgamma[col] = (float)red[1][0][k];
+  }
+}
+
 // dx for the channels [col0, col0 + cols), col0 a multiple of the piece (so that
 // one lies in one block).
-template <typename T>
+template <typename T, bool CUT>
 __global__ __launch_bounds__(kThreads) void k_input_q8_pieces(
     const T* __restrict__ da, int64_t ldd, const int8_t* __restrict__ codes, const uint8_t* __restrict__ exponents,
     int64_t n, int c, int blocks, int col0, int cols, const float* __restrict__ gamma, const float* __restrict__ beta,
     const float* __restrict__ invstd, const float* __restrict__ dgamma, const float* __restrict__ dbeta,
     const T* __restrict__ add, int64_t lda, T* __restrict__ dx, int64_t ldo) {
   constexpr int P = kPiece<T>;
-  Place<P> w(cols, (cols + kBlock - 1) / kBlock);
+  const Place<P> w(cols, (cols + kBlock - 1) / kBlock);
   if (w.valid == 0) return;
-  const int k = w.col;  // first channel of the range's own columns
-  w.col += col0;
+  const int col = col0 + w.col;  // of the layer
   const float inv_n = 1.f / (float)n;
   float ga[P], be[P], m0[P], m1[P], gi[P];
-  load_piece<P>(gamma + w.col, w.valid, ga);
-  load_piece<P>(beta + w.col, w.valid, be);
-  load_piece<P>(dbeta + w.col, w.valid, m0);
-  load_piece<P>(dgamma + w.col, w.valid, m1);
-  load_piece<P>(invstd + w.col, w.valid, gi);
+  constants<P>(gamma + col, w.valid, ga);
+  constants<P>(beta + col, w.valid, be);
+  constants<P>(dbeta + col, w.valid, m0);
+  constants<P>(dgamma + col, w.valid, m1);
+  constants<P>(invstd + col, w.valid, gi);
 #pragma unroll
   for (int i = 0; i < P; ++i) {
     m0[i] *= inv_n;
     m1[i] *= inv_n;
     gi[i] *= ga[i];
   }
-  const uint8_t* exps = exponents + w.col / kBlock;
-  for (int64_t r = w.row; r < n; r += w.step) {
-    float d[P], v[P], out[P];
-    load_piece(da + r * ldd + w.col, w.valid, d);
-    decode_piece(codes + r * c + w.col, w.valid, exps[r * blocks], v);
-    if (add) load_piece(add + r * lda + k, w.valid, out);
+  for (int64_t r0 = w.row; r0 < n; r0 += kRows * w.step) {
+    const Turn<T, CUT> t(w, r0, n, codes + col, c, exponents + col / kBlock, blocks, da + col, ldd);
+    uint32_t more[kRows][4];
+    if (add) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) {
-      const float dz = pre_restored(v[i], ga[i], be[i]) > 0.f ? d[i] : 0.f;
-      const float g = gi[i] * (dz - m0[i] - v[i] * m1[i]);
-      out[i] = add ? g + out[i] : g;
+      for (int u = 0; u < kRows; ++u) {
+        const int64_t r = r0 + u * w.step;
+        load_piece<T, CUT>(add + r * lda + w.col, r < n ? w.valid : 0, more[u]);
+      }
     }
-    store_piece(dx + r * ldo + k, w.valid, out);
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+      const int64_t r = r0 + u * w.step;
+      if (r >= n) break;
+      float v[P], out[P];
+      decode<P>(t.q[u], t.byte[u], v);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const float dz = pre_restored(v[i], ga[i], be[i]) > 0.f ? value<P>(t.d[u], i) : 0.f;
+        out[i] = gi[i] * (dz - m0[i] - v[i] * m1[i]);
+        if (add) out[i] += value<P>(more[u], i);
+      }
+      store_piece<T, CUT>(dx + r * ldo + w.col, w.valid, out);
+    }
   }
 }
 
@@ -331,6 +430,21 @@ dim3 place_grid(int64_t n, int blocks, int64_t most, sscn_dtype dtype) {
 // Workgroups over the rows of the row-wise kernels: 256 CUs hold some 6 each.
 constexpr int64_t kRowGroups = 2048;
 
+// f(a value of the element type, whether rows of `cols` channels have a cut piece).
+template <class F>
+sscn_status by_type(sscn_dtype dtype, int cols, const F& f) {
+  const bool cut = cols % piece_of(dtype) != 0;
+  if (dtype == SSCN_F32) {
+    if (cut) f(float{}, std::true_type{});
+    else f(float{}, std::false_type{});
+  } else {
+    if (cut) f(uint16_t{}, std::true_type{});
+    else f(uint16_t{}, std::false_type{});
+  }
+  SSCN_HIP(hipGetLastError());
+  return SSCN_OK;
+}
+
 sscn_status check_dtype(sscn_dtype dtype) {
   if (dtype != SSCN_F32 && dtype != SSCN_BF16) return fail(SSCN_ERR_INVALID_ARG, "unknown dtype");
   return SSCN_OK;
@@ -367,14 +481,11 @@ extern "C" sscn_status sscn_batchnorm_relu_apply_q8(const void* x, int64_t ldx, 
   if (n == 0) return SSCN_OK;
   const int blocks = (int)ceil_div(c, kBlock);
   const dim3 g = place_grid(n, blocks, kRowGroups, dtype);
-  if (dtype == SSCN_F32)
-    k_apply_q8<float><<<g, 256, 0, stream>>>((const float*)x, ldx, n, c, blocks, mean, invstd, scale, gamma, beta,
-                                             (float*)y, ldy, codes, exponents);
-  else
-    k_apply_q8<uint16_t><<<g, 256, 0, stream>>>((const uint16_t*)x, ldx, n, c, blocks, mean, invstd, scale, gamma,
-                                                beta, (uint16_t*)y, ldy, codes, exponents);
-  SSCN_HIP(hipGetLastError());
-  return SSCN_OK;
+  return by_type(dtype, c, [&](auto t, auto cut) {
+    using T = decltype(t);
+    k_apply_q8<T, decltype(cut)::value><<<g, kThreads, 0, stream>>>((const T*)x, ldx, n, c, blocks, mean, invstd, scale,
+                                                                    gamma, beta, (T*)y, ldy, codes, exponents);
+  });
 }
 
 extern "C" sscn_status sscn_q8_values(const int8_t* codes, const uint8_t* exponents, int64_t n, int32_t c,
@@ -385,12 +496,10 @@ extern "C" sscn_status sscn_q8_values(const int8_t* codes, const uint8_t* expone
   if (n == 0) return SSCN_OK;
   const int blocks = (int)ceil_div(c, kBlock);
   const dim3 g = place_grid(n, blocks, kRowGroups, dtype);
-  if (dtype == SSCN_F32)
-    k_q8_values<float><<<g, 256, 0, stream>>>(codes, exponents, n, c, blocks, (float*)y, ldy);
-  else
-    k_q8_values<uint16_t><<<g, 256, 0, stream>>>(codes, exponents, n, c, blocks, (uint16_t*)y, ldy);
-  SSCN_HIP(hipGetLastError());
-  return SSCN_OK;
+  return by_type(dtype, c, [&](auto t, auto cut) {
+    using T = decltype(t);
+    k_q8_values<T, decltype(cut)::value><<<g, kThreads, 0, stream>>>(codes, exponents, n, c, blocks, (T*)y, ldy);
+  });
 }
 
 extern "C" sscn_status sscn_batchnorm_relu_backward_params_q8_workspace(int64_t n, int32_t c, int64_t* bytes) {
@@ -420,14 +529,12 @@ extern "C" sscn_status sscn_batchnorm_relu_backward_params_q8(const void* da, in
   const dim3 grid = place_grid(n, blocks, kMaxPartials, dtype);
   const int parts = (int)grid.x;
   double* partial = (double*)workspace;
-  if (dtype == SSCN_F32)
-    k_params_q8<float><<<grid, 256, 0, stream>>>((const float*)da, ldd, codes, exponents, n, c, blocks, gamma, beta,
-                                                 (float*)a, lda, partial);
-  else
-    k_params_q8<uint16_t><<<grid, 256, 0, stream>>>((const uint16_t*)da, ldd, codes, exponents, n, c, blocks, gamma,
-                                                    beta, (uint16_t*)a, lda, partial);
-  SSCN_HIP(hipGetLastError());
-  k_two_sums<<<(unsigned)ceil_div(c, 64), kFinThreads, 0, stream>>>(partial, parts, c, dbeta, dgamma);
+  SSCN_TRY(by_type(dtype, c, [&](auto t, auto cut) {
+    using T = decltype(t);
+    k_params_q8<T, decltype(cut)::value><<<grid, kThreads, 0, stream>>>((const T*)da, ldd, codes, exponents, n, c,
+                                                                        blocks, gamma, beta, (T*)a, lda, partial);
+  }));
+  k_sum_parts<<<(unsigned)ceil_div(c, 16), 1024, 0, stream>>>(partial, parts, c, dbeta, dgamma);
   SSCN_HIP(hipGetLastError());
   return SSCN_OK;
 }
@@ -452,16 +559,12 @@ extern "C" sscn_status sscn_batchnorm_relu_backward_input_q8(const void* da, int
   const int blocks = (int)ceil_div(c, kBlock);
   if (col0 % piece_of(dtype) == 0) {
     const dim3 g = place_grid(n, (int)ceil_div(cols, kBlock), kRowGroups, dtype);
-    if (dtype == SSCN_F32)
-      k_input_q8_pieces<float><<<g, kThreads, 0, stream>>>((const float*)da, ldd, codes, exponents, n, c, blocks, col0,
-                                                           cols, gamma, beta, invstd, dgamma, dbeta,
-                                                           (const float*)add, ld_add, (float*)dx, ldx_out);
-    else
-      k_input_q8_pieces<uint16_t><<<g, kThreads, 0, stream>>>(
-          (const uint16_t*)da, ldd, codes, exponents, n, c, blocks, col0, cols, gamma, beta, invstd, dgamma, dbeta,
-          (const uint16_t*)add, ld_add, (uint16_t*)dx, ldx_out);
-    SSCN_HIP(hipGetLastError());
-    return SSCN_OK;
+    return by_type(dtype, cols, [&](auto t, auto cut) {
+      using T = decltype(t);
+      k_input_q8_pieces<T, decltype(cut)::value><<<g, kThreads, 0, stream>>>(
+          (const T*)da, ldd, codes, exponents, n, c, blocks, col0, cols, gamma, beta, invstd, dgamma, dbeta,
+          (const T*)add, ld_add, (T*)dx, ldx_out);
+    });
   }
   const unsigned g = grid_of(ceil_div(n * cols, 256));
   if (dtype == SSCN_F32)

@@ -16,7 +16,6 @@
 
 #include "internal.h"
 #include "numeric.h"
-#include "partials.h"
 #include "sgd_batch.h"
 
 namespace sscn {
@@ -205,6 +204,44 @@ __global__ __launch_bounds__(256) void k_colreduce_vec(const T* __restrict__ x, 
   }
 }
 
+// Sums of the partials of the `blocks` workgroups for channel col: one
+// workgroup of kFinThreads threads per 64 channels, wavefront w adding
+// blocks w, w + 16, .. in order, then the sixteen wavefronts' sums added
+// pairwise in a fixed tree (a fixed order: reproducible).  (One thread
+// adding all blocks in turn took ~0.25 ms for 1024 blocks; four wavefronts
+// ~15 us.)
+constexpr int kFinThreads = 1024;
+__device__ __forceinline__ bool sum_partials(const double* __restrict__ partial, int blocks, int c, double& s0,
+                                             double& s1, int& col) {
+  constexpr int NW = kFinThreads / 64;
+  __shared__ double red[2][NW][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  col = blockIdx.x * 64 + lane;
+  double a0 = 0.0, a1 = 0.0;
+  if (col < c) {
+#pragma unroll 4
+    for (int b = wave; b < blocks; b += NW) {
+      a0 += partial[((int64_t)b * 2) * c + col];
+      a1 += partial[((int64_t)b * 2 + 1) * c + col];
+    }
+  }
+  red[0][wave][lane] = a0;
+  red[1][wave][lane] = a1;
+  __syncthreads();
+#pragma unroll
+  for (int h = NW / 2; h >= 1; h /= 2) {
+    if (wave < h) {
+      red[0][wave][lane] += red[0][wave + h][lane];
+      red[1][wave][lane] += red[1][wave + h][lane];
+    }
+    __syncthreads();
+  }
+  if (wave != 0 || col >= c) return false;
+  s0 = red[0][0][lane];
+  s1 = red[1][0][lane];
+  return true;
+}
+
 // Batch statistics -> the affine map of the normalisation, and the running
 // (inference) statistics: mean, biased variance for the map, unbiased for
 // the running variance.
@@ -230,6 +267,15 @@ __global__ __launch_bounds__(kFinThreads) void k_bn_finalize(const double* __res
     running_mean[col] = (1.f - momentum) * running_mean[col] + momentum * (float)mu;
     running_var[col] = (1.f - momentum) * running_var[col] + momentum * (float)unbiased;
   }
+}
+
+__global__ __launch_bounds__(kFinThreads) void k_two_sums(const double* __restrict__ partial, int blocks, int c,
+                                                  float* __restrict__ out0, float* __restrict__ out1) {
+  double s0, s1;
+  int col;
+  if (!sum_partials(partial, blocks, c, s0, s1, col)) return;
+  out0[col] = (float)s0;
+  if (out1) out1[col] = (float)s1;
 }
 
 // dx = gamma invstd (dz - dbeta / n - xhat dgamma / n) (+ add), dz = dA where
