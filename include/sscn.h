@@ -477,7 +477,8 @@ sscn_status sscn_softmax_nll(const void* logits, int64_t n, int32_t classes, ssc
  *                      ties to the lowest class, NaN above everything
  *   top_logprob[r][j]  its log p
  *   logits   n x classes in dtype, row stride ldz >= classes, any alignment
- *            of its elements' size
+ *            of its elements' size (values between the rows may be read, and
+ *            have no effect)
  *   labels   device int32, n; NULL with logprob NULL: no labels
  *   top_k    0 .. min(16, classes); 0: top_index and top_logprob are not used
  * Numbers are computed and written in fp32.  A class of logit -inf is
@@ -538,7 +539,7 @@ sscn_status sscn_label_scores_backward(const void* logits, int64_t ldz, int64_t 
 
 /*
  * sscn_batchnorm_relu_apply_q8 -- sscn_batchnorm_relu_apply (the same y, bit
- * for bit; y may be x) that also writes codes and exponents.  mean, invstd
+ * for bit; y may be x, with its row stride) that also writes codes and exponents.  mean, invstd
  * and scale are those of sscn_batchnorm_forward.
  */
 sscn_status sscn_batchnorm_relu_apply_q8(const void* x, int64_t ldx, int64_t n, int32_t c, sscn_dtype dtype,
@@ -573,7 +574,8 @@ sscn_status sscn_batchnorm_relu_backward_params_q8_workspace(int64_t n, int32_t 
  *   dx = gamma * invstd * (dz - dbeta / n - xhat' * dgamma / n)  (+ add),
  * for the channels [col0, col0 + cols) of the layer.  dA, the codes, the
  * exponents and the vectors are the whole layer's (c channels); add
- * (nullable) and dx hold the range's columns alone.  dx may be add.
+ * (nullable) and dx hold the range's columns alone.  dx may be add (the same
+ * row stride), not dA.
  */
 sscn_status sscn_batchnorm_relu_backward_input_q8(const void* dA, int64_t ldd, const int8_t* codes,
                                                   const uint8_t* exponents, int64_t n, int32_t c, int32_t col0,

@@ -283,8 +283,10 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
           if (mask == 0) continue;
           if constexpr (L < 64) mask = mask >> (team * L) & ((1ull << L) - 1);
           if (in) {
-            const int at = count + (L < 64 ? __popc((uint32_t)mask & ((1u << lane) - 1))
-                                           : (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)));
+            const int before = L < 64 ? __popc((uint32_t)mask & ((1u << lane) - 1))
+                                      : (int)__builtin_amdgcn_mbcnt_hi(
+                                            (uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+            const int at = count + before;
             if (at < kList) list[at] = rank_key(v, (uint32_t)(k0 + x.place(g) + i));
           }
           count += __popcll(mask);
@@ -443,6 +445,7 @@ __global__ __launch_bounds__(64) void k_scores_join(const T* __restrict__ z, int
 // insertion: bf16 as keys that hold the class too, one operation a place (a
 // value, class pair takes four); fp32 by strict comparisons from the lowest
 // class up, so that ties stay in order.  The first is left out of t.
+
 // A row of more than NP and at most NC classes as fp32, -inf past its end, in
 // pieces of 16 bytes.  A cut last piece runs into what follows the row (and is
 // cut off below); where that is the end of the matrix, `last`, pieces are moved
@@ -524,13 +527,13 @@ __global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int
     groups_of_4<NP, NC>(classes, [&](auto k0) {
 #pragma unroll
       for (int k = k0; k < k0 + 4; ++k) {
-          m = OpMax::of(m, x[k]);
-          const int32_t bits = (int32_t)__float_as_uint(x[k] + 0.f);  // -0 is 0
-          const int32_t in = (bits ^ ((bits >> 31) & 0x7fff0000)) + (NC - 1 - k);
+        m = OpMax::of(m, x[k]);
+        const int32_t bits = (int32_t)__float_as_uint(x[k] + 0.f);  // -0 is 0
+        const int32_t in = (bits ^ ((bits >> 31) & 0x7fff0000)) + (NC - 1 - k);
 #pragma unroll
-          for (int j = KT - 1; j > 0; --j) key[j] = middle(in, key[j - 1], key[j]);
-          key[0] = max(key[0], in);
-        }
+        for (int j = KT - 1; j > 0; --j) key[j] = middle(in, key[j - 1], key[j]);
+        key[0] = max(key[0], in);
+      }
     });
 #pragma unroll
     for (int j = 0; j < KT; ++j) {
@@ -547,19 +550,19 @@ __global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int
     groups_of_4<NP, NC>(classes, [&](auto k0) {
 #pragma unroll
       for (int k = k0; k < k0 + 4; ++k) {
-          const float v = x[k];  // -inf past the end: above nothing
-          m = OpMax::of(m, v);
-          bool above[KT];
+        const float v = x[k];  // -inf past the end: above nothing
+        m = OpMax::of(m, v);
+        bool above[KT];
 #pragma unroll
-          for (int j = 0; j < KT; ++j) above[j] = v > tv[j];
+        for (int j = 0; j < KT; ++j) above[j] = v > tv[j];
 #pragma unroll
-          for (int j = KT - 1; j > 0; --j) {
-            ti[j] = above[j - 1] ? ti[j - 1] : above[j] ? k : ti[j];
-            tv[j] = __builtin_amdgcn_fmed3f(v, tv[j - 1], tv[j]);
-          }
-          ti[0] = above[0] ? k : ti[0];
-          tv[0] = fmaxf(tv[0], v);
+        for (int j = KT - 1; j > 0; --j) {
+          ti[j] = above[j - 1] ? ti[j - 1] : above[j] ? k : ti[j];
+          tv[j] = __builtin_amdgcn_fmed3f(v, tv[j - 1], tv[j]);
         }
+        ti[0] = above[0] ? k : ti[0];
+        tv[0] = fmaxf(tv[0], v);
+      }
     });
   }
   ExpSums sum(m);
@@ -1023,6 +1026,7 @@ extern "C" sscn_status sscn_label_scores_backward(const void* logits, int64_t ld
   if (dlogprob && !labels) return fail(SSCN_ERR_INVALID_ARG, "scores: dlogprob without labels");
   if (dentropy && !entropy) return fail(SSCN_ERR_INVALID_ARG, "scores: dentropy without entropy");
   if (dtop && (top_k == 0 || !top_index)) return fail(SSCN_ERR_INVALID_ARG, "scores: dtop without top_index");
+  if (dlogits == logits) return fail(SSCN_ERR_INVALID_ARG, "scores: the gradient cannot replace the logits");
   const GradInputs q{labels, stats, entropy, dtop ? top_k : 0, top_index, dlogprob, dentropy, dtop};
   return dtype == SSCN_F32 ? launch_grad((const float*)logits, ldz, n, classes, q, (float*)dlogits, ldd, stream)
                            : launch_grad((const uint16_t*)logits, ldz, n, classes, q, (uint16_t*)dlogits, ldd, stream);

@@ -8,7 +8,7 @@ import torch
 from paper_1711_10275_amd import sscn
 
 INVALID = sscn.STATUS_CODES["invalid_arg"]
-P = ctypes.c_void_p(4096)      # never read: every call below is refused or has no rows
+P, Q = ctypes.c_void_p(4096), ctypes.c_void_p(8192)      # never read: every call below is refused or has no rows
 
 
 def _scores(z=P, ldz=8, n=4, k=8, dtype=0, labels=P, top_k=2, logprob=P, entropy=P, stats=P, index=P, top=P, work=P,
@@ -17,7 +17,7 @@ def _scores(z=P, ldz=8, n=4, k=8, dtype=0, labels=P, top_k=2, logprob=P, entropy
                                         work_bytes, None)
 
 
-def _scores_back(z=P, ldz=8, n=4, k=8, dtype=0, labels=P, stats=P, entropy=P, top_k=2, index=P, g=P, h=P, t=P, d=P,
+def _scores_back(z=P, ldz=8, n=4, k=8, dtype=0, labels=P, stats=P, entropy=P, top_k=2, index=P, g=P, h=P, t=P, d=Q,
                  ldd=8):
     return sscn.lib().sscn_label_scores_backward(z, ldz, n, k, dtype, labels, stats, entropy, top_k, index, g, h, t, d,
                                                  ldd, None)
@@ -33,7 +33,7 @@ def test_label_scores_refuses(bad):
 
 @pytest.mark.parametrize("bad", [dict(z=None), dict(ldz=7), dict(ldd=7), dict(n=-1), dict(dtype=-1), dict(top_k=9),
                                  dict(labels=None), dict(stats=None), dict(entropy=None), dict(index=None),
-                                 dict(top_k=0), dict(d=None), dict(d=ctypes.c_void_p(4097))])
+                                 dict(top_k=0), dict(d=None), dict(d=ctypes.c_void_p(4097)), dict(d=P)])
 def test_label_scores_backward_refuses(bad):
     assert _scores_back(**bad) == INVALID and sscn.lib().sscn_last_error()
 
@@ -54,16 +54,16 @@ def test_workspaces():
         assert _scores(n=1, k=1 << 20, ldz=1 << 20, top_k=8, work=None) == INVALID
 
 
-def _apply(x=P, ldx=40, n=4, c=40, dtype=0, mean=P, gamma=P, y=P, ldy=40, codes=P, exps=P):
+def _apply(x=P, ldx=40, n=4, c=40, dtype=0, mean=P, gamma=P, y=Q, ldy=40, codes=P, exps=P):
     return sscn.lib().sscn_batchnorm_relu_apply_q8(x, ldx, n, c, dtype, mean, P, P, gamma, P, y, ldy, codes, exps, None)
 
 
-def _params(d=P, ldd=40, n=4, c=40, dtype=0, codes=P, exps=P, gamma=P, dg=P, a=P, lda=40, work=P, work_bytes=1 << 40):
+def _params(d=P, ldd=40, n=4, c=40, dtype=0, codes=P, exps=P, gamma=P, dg=P, a=Q, lda=40, work=P, work_bytes=1 << 40):
     return sscn.lib().sscn_batchnorm_relu_backward_params_q8(d, ldd, codes, exps, n, c, dtype, gamma, P, dg, P, a, lda,
                                                              work, work_bytes, None)
 
 
-def _input(d=P, ldd=40, n=4, c=40, col0=0, cols=40, dtype=0, codes=P, gamma=P, dg=P, add=P, lda=40, dx=P, ldo=40):
+def _input(d=P, ldd=40, n=4, c=40, col0=0, cols=40, dtype=0, codes=P, gamma=P, dg=P, add=P, lda=40, dx=Q, ldo=40):
     return sscn.lib().sscn_batchnorm_relu_backward_input_q8(d, ldd, codes, P, n, c, col0, cols, dtype, gamma, P, P, dg,
                                                             P, add, lda, dx, ldo, None)
 
@@ -71,7 +71,8 @@ def _input(d=P, ldd=40, n=4, c=40, col0=0, cols=40, dtype=0, codes=P, gamma=P, d
 @pytest.mark.parametrize("call,bad", [
     (_apply, dict(x=None)), (_apply, dict(ldx=39)), (_apply, dict(ldy=39)), (_apply, dict(n=-1)), (_apply, dict(c=0)),
     (_apply, dict(dtype=2)), (_apply, dict(mean=None)), (_apply, dict(gamma=None)), (_apply, dict(codes=None)),
-    (_apply, dict(exps=None)), (_apply, dict(x=ctypes.c_void_p(4098))),
+    (_apply, dict(exps=None)), (_apply, dict(x=ctypes.c_void_p(4098))), (_apply, dict(y=P, ldy=41)),
+    (_params, dict(a=P)), (_input, dict(dx=P)), (_input, dict(add=Q, lda=41)),
     (_params, dict(d=None)), (_params, dict(ldd=39)), (_params, dict(codes=None)), (_params, dict(gamma=None)),
     (_params, dict(dg=None)), (_params, dict(lda=39)), (_params, dict(work=None)), (_params, dict(work_bytes=8)),
     (_params, dict(work=ctypes.c_void_p(4100))), (_params, dict(dtype=7)),
