@@ -389,50 +389,102 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
   }
 }
 
-// Joins the parts of a row, one wavefront per row.  Lane l takes the parts l,
-// l + 64, ..; the best classes come off the heads of 64 of the parts' lists, or
-// of 63 more and of the list so far (lane 63).
+// Joins the parts of a row, one wavefront per row; lane l has the parts l, l +
+// 64, .. .  The best classes of up to 64 parts: keys below the top_k-th best of
+// the lists' heads (as in k_scores_chunk) are out, the others are ranked.  Of
+// more parts, or where more than kRanked keys are left, they come off the heads
+// one by one: of 64 lists, or of 63 more and of the list so far (lane 63).
 template <typename T>
 __global__ __launch_bounds__(64) void k_scores_join(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
                                                     int parts, const int32_t* __restrict__ labels, int top_k,
                                                     Outputs o, const float4* __restrict__ part_in,
                                                     const uint64_t* __restrict__ keys_in) {
-  __shared__ uint64_t list[64 * kMaxTop], top[kMaxTop];
+  constexpr int kRanked = 128;
+  __shared__ uint64_t list[64 * kMaxTop], left[kRanked], top[kMaxTop];
   const int lane = threadIdx.x;
   for (int64_t r = blockIdx.x; r < n; r += gridDim.x) {
+    // what the row needs from memory, all of it before the first wait
+    const int first = min(parts, 64) * top_k;  // keys of the first 64 parts
+    uint64_t key[kMaxTop];
+#pragma unroll
+    for (int i = 0; i < kMaxTop; ++i) {
+      if (i * 64 >= first) break;
+      key[i] = lane + i * 64 < first ? keys_in[r * parts * top_k + lane + i * 64] : 0;
+    }
+    const Label lab = label_of(z + r * ldz, labels, r, classes);
     Part p{-INFINITY, 0.f, 0.f};
     for (int c = lane; c < parts; c += 64) {
       const float4 q = part_in[r * parts + c];
-      p = join(p, Part{q.x, q.y, q.z});
+      p = c < 64 ? Part{q.x, q.y, q.z} : join(p, Part{q.x, q.y, q.z});
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const Part q{__shfl_xor(p.m, d, 64), __shfl_xor(p.t, d, 64), __shfl_xor(p.a, d, 64)};
-      p = (lane & d) ? join(q, p) : join(p, q);  // the lower lane's part first: every lane the same
-    }
+    // the lanes' parts: values below the maximum shift by d, and of several
+    // parts that hold it one goes without it
+    const float m = wave_reduce<OpMax>(p.m), d = p.m - m;
+    const bool holds = p.m == m, some = p.m > -INFINITY;
+    const float e = expf(d), all = 1.f + p.t;
+    const float t = wave_reduce<OpAdd>(holds ? p.t : some ? e * all : 0.f);
+    const float a = wave_reduce<OpAdd>(holds ? p.a : some ? e * (p.a + fmaxf(d, -200.f) * all) : 0.f);
+    const Part row{m, m == -INFINITY ? 0.f : t + (float)(__popcll(__ballot(holds)) - 1), m == -INFINITY ? 0.f : a};
     if (lane < kMaxTop) top[lane] = 0;
+#pragma unroll
+    for (int i = 0; i < kMaxTop; ++i) {
+      if (i * 64 >= first) break;
+      list[lane + i * 64] = key[i];
+    }
     __syncthreads();
     if (top_k > 0) {
-      for (int c0 = 0; c0 < parts;) {
-        const int lists = min(parts - c0, c0 == 0 ? 64 : 63), carry = c0 == 0 ? 0 : 1;
-        const uint64_t* from = keys_in + (r * parts + c0) * top_k;
-        for (int i = lane; i < lists * top_k; i += 64) list[i] = from[i];
-        if (carry && lane < top_k) list[63 * kMaxTop + lane] = top[lane];
-        __syncthreads();
-        const uint64_t* mine = lane < lists ? list + lane * top_k : list + 63 * kMaxTop;
-        const bool have = lane < lists || (carry && lane == 63);
-        uint64_t head = have ? mine[0] : 0;
-        int at = 0;  // entries taken off this lane's list
-        for (int j = 0; j < top_k; ++j) {
-          const uint64_t win = wave_max_key(head);
-          if (lane == 0) top[j] = win;
-          if (win != 0 && head == win) head = ++at < top_k ? mine[at] : 0;
+      int count = 0;
+      if (parts <= 64) {
+        const uint32_t head = lane < parts ? (uint32_t)(list[lane * top_k] >> 32) : 0;
+        const float v = head == 0 ? -INFINITY : head == 0xfffffffeu ? INFINITY : key_value((uint64_t)head << 32);
+        const float cut = wave_reduce<OpMin>(above_in_row(v, v) < (top_k + 3) / 4 ? v : INFINITY);
+        const uint32_t least = (uint32_t)(rank_key(cut, 0) >> 32);
+#pragma unroll
+        for (int i = 0; i < kMaxTop; ++i) {
+          if (i * 64 >= first) break;
+          const bool in = key[i] != 0 && (uint32_t)(key[i] >> 32) >= least;
+          const uint64_t mask = __ballot(in);
+          if (in) {
+            const int at = count + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32),
+                                                                  __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+            if (at < kRanked) left[at] = key[i];
+          }
+          count += __popcll(mask);
         }
         __syncthreads();
-        c0 += lists;
+      }
+      if (parts <= 64 && count <= kRanked) {
+        for (int i = lane; i < count; i += 64) {
+          const uint64_t own = left[i];
+          int above = 0;
+          for (int j = 0; j < count; ++j) above += left[j] > own;
+          if (above < top_k) top[above] = own;
+        }
+        __syncthreads();
+      } else {
+        for (int c0 = 0; c0 < parts;) {
+          const int lists = min(parts - c0, c0 == 0 ? 64 : 63), carry = c0 == 0 ? 0 : 1;
+          if (carry) {
+            const uint64_t* from = keys_in + (r * parts + c0) * top_k;
+            for (int i = lane; i < lists * top_k; i += 64) list[i] = from[i];
+            if (lane < top_k) list[63 * kMaxTop + lane] = top[lane];
+            __syncthreads();
+          }
+          const uint64_t* mine = lane < lists ? list + lane * top_k : list + 63 * kMaxTop;
+          const bool have = lane < lists || (carry && lane == 63);
+          uint64_t head = have ? mine[0] : 0;
+          int at = 0;  // entries taken off this lane's list
+          for (int j = 0; j < top_k; ++j) {
+            const uint64_t win = wave_max_key(head);
+            if (lane == 0) top[j] = win;
+            if (win != 0 && head == win) head = ++at < top_k ? mine[at] : 0;
+          }
+          __syncthreads();
+          c0 += lists;
+        }
       }
     }
-    write_row(lane, r, label_of(z + r * ldz, labels, r, classes), top_k, p, top, o);
+    write_row(lane, r, lab, top_k, row, top, o);
     __syncthreads();
   }
 }
