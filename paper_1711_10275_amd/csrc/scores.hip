@@ -199,7 +199,7 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
   // keys that a wavefront's part of a team may list, and may rank
   constexpr int kList = L == 16 ? 128 : L * E < 512 ? L * E : 512, kRanked = 128 / W;
   __shared__ uint64_t lists[kTeams * W][kList], tops[kTeams][kMaxTop], most[2][W];
-  __shared__ float red[2][W], sums[3][W];
+  __shared__ float red[4 * W], sums[3][W];
   __shared__ int counts[W];
   static_assert(W == 1 || (W == 4 && L == 64));
   const int wave = threadIdx.x >> 6;
@@ -234,9 +234,9 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
       half1 = OpMax::of(half1, m1);
     }
     const float own = OpMax::of(half0, half1);
-    // the threshold: of 16 lanes the top_k-th largest maximum (of 64 lanes, the
-    // least of the four rows' top_k / 4-th), or of the maxima of groups
-    float m = wave_reduce<OpMax, 1, L>(own), cut = m;
+    // the threshold: the top_k-th largest of 16 lanes' maxima (of 64 lanes, the
+    // least of the four rows' top_k / 4-th; of four wavefronts, of 16 rows' maxima)
+    float m = W == 1 ? wave_reduce<OpMax, 1, L>(own) : 0.f, cut = m;
     if constexpr (KT == 0) {
     } else if constexpr (L == 16) {
       if (KT > 8 && top_k > 8) {
@@ -249,25 +249,17 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
       }
     } else if constexpr (W == 1) {
       if (top_k > 1) cut = wave_reduce<OpMin>(above_in_row(own, own) < (top_k + 3) / 4 ? own : INFINITY);
-    } else if (top_k > 4) {
-      const float v16 = wave_reduce<OpMax, 1, 16>(own);
-      cut = wave_reduce<OpMin, 16, 64>(top_k <= 8 ? wave_reduce<OpMax, 16, 32>(v16) : v16);
     }
     if (all < kMaxTop) top[all] = 0;
     if constexpr (W > 1) {
-      if (lane == 0) {
-        red[0][wave] = m;
-        red[1][wave] = cut;
-      }
+      const float v16 = wave_reduce<OpMax, 1, 16>(own);
+      if (lane % 16 == 0) red[threadIdx.x / 16] = v16;
     }
     __syncthreads();
     if constexpr (W > 1) {
-      const float m0 = red[0][0], m1 = red[0][1], m2 = red[0][2], m3 = red[0][3];
-      m = OpMax::of(OpMax::of(m0, m1), OpMax::of(m2, m3));
-      const float least = fminf(fminf(red[1][0], red[1][1]), fminf(red[1][2], red[1][3]));
-      // of four maxima the first, second, third or fourth largest
-      const float mid0 = fminf(fmaxf(m0, m1), fmaxf(m2, m3)), mid1 = fmaxf(fminf(m0, m1), fminf(m2, m3));
-      cut = top_k == 1 ? m : top_k == 2 ? fmaxf(mid0, mid1) : top_k == 3 ? fminf(mid0, mid1) : least;
+      const float v = red[lane % 16];
+      m = wave_reduce<OpMax, 1, 16>(v);
+      if (KT > 0) cut = wave_reduce<OpMin, 1, 16>(above_in_row(v, v) < top_k ? v : INFINITY);
     }
     int count = 0;  // keys listed by this wavefront's part of the team
     cut = fmaxf(cut, -3.402823466e38f);  // -inf stays out
