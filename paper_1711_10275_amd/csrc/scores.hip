@@ -175,6 +175,14 @@ __device__ __forceinline__ void write_row(int lane, int64_t r, const Label& lab,
   }
 }
 
+// The k-th largest of the 32 values v0, v1 of the 16 lanes of each row.
+__device__ __forceinline__ float kth_of_32(float v0, float v1, int k) {
+  const float hi = fmaxf(v0, v1), lo = fminf(v0, v1);
+  const int above_hi = above_in_row(hi, hi) + above_in_row(lo, hi);
+  const int above_lo = above_in_row(hi, lo) + above_in_row(lo, lo) + (hi > lo);
+  return wave_reduce<OpMin, 1, 16>(above_lo < k ? lo : above_hi < k ? hi : INFINITY);
+}
+
 // Teams of W wavefronts (W = 1: 64 / L teams to a workgroup of one wavefront,
 // a whole row each; W = 4: L = 64 lanes of each wavefront together, one chunk
 // of one row, blockIdx.x the chunk).  Where a row is one chunk it is written,
@@ -199,7 +207,7 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
   // keys that a wavefront's part of a team may list, and may rank
   constexpr int kList = L == 16 ? 128 : L * E < 512 ? L * E : 512, kRanked = 128 / W;
   __shared__ uint64_t lists[kTeams * W][kList], tops[kTeams][kMaxTop], most[2][W];
-  __shared__ float red[4 * W], sums[3][W];
+  __shared__ float red[8 * W], sums[3][W];
   __shared__ int counts[W];
   static_assert(W == 1 || (W == 4 && L == 64));
   const int wave = threadIdx.x >> 6;
@@ -234,16 +242,14 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
       half1 = OpMax::of(half1, m1);
     }
     const float own = OpMax::of(half0, half1);
-    // the threshold: the top_k-th largest of 16 lanes' maxima (of 64 lanes, the
-    // least of the four rows' top_k / 4-th; of four wavefronts, of 16 rows' maxima)
+    // the threshold: the top_k-th largest of 16 maxima, of 32 for more than 8
+    // (lanes or their halves, of four wavefronts rows of lanes or their halves; of
+    // one wavefront the least of its four rows' top_k / 4-th largest)
     float m = W == 1 ? wave_reduce<OpMax, 1, L>(own) : 0.f, cut = m;
     if constexpr (KT == 0) {
     } else if constexpr (L == 16) {
       if (KT > 8 && top_k > 8) {
-        const float lo = fminf(half0, half1);  // own and lo, of each lane
-        const int above_own = above_in_row(own, own) + above_in_row(lo, own);
-        const int above_lo = above_in_row(own, lo) + above_in_row(lo, lo) + (own > lo);
-        cut = wave_reduce<OpMin, 1, 16>(above_lo < top_k ? lo : above_own < top_k ? own : INFINITY);
+        cut = kth_of_32(half0, half1, top_k);
       } else if (top_k > 1) {
         cut = wave_reduce<OpMin, 1, 16>(above_in_row(own, own) < top_k ? own : INFINITY);
       }
@@ -252,14 +258,15 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
     }
     if (all < kMaxTop) top[all] = 0;
     if constexpr (W > 1) {
-      const float v16 = wave_reduce<OpMax, 1, 16>(own);
-      if (lane % 16 == 0) red[threadIdx.x / 16] = v16;
+      const float v8 = wave_reduce<OpMax, 1, 8>(own);
+      if (lane % 8 == 0) red[threadIdx.x / 8] = v8;
     }
     __syncthreads();
     if constexpr (W > 1) {
-      const float v = red[lane % 16];
+      const float v0 = red[2 * (lane % 16)], v1 = red[2 * (lane % 16) + 1], v = OpMax::of(v0, v1);
       m = wave_reduce<OpMax, 1, 16>(v);
-      if (KT > 0) cut = wave_reduce<OpMin, 1, 16>(above_in_row(v, v) < top_k ? v : INFINITY);
+      if (KT > 8 && top_k > 8) cut = kth_of_32(v0, v1, top_k);
+      else if (KT > 0) cut = wave_reduce<OpMin, 1, 16>(above_in_row(v, v) < top_k ? v : INFINITY);
     }
     int count = 0;  // keys listed by this wavefront's part of the team
     cut = fmaxf(cut, -3.402823466e38f);  // -inf stays out
