@@ -197,6 +197,13 @@ __device__ __forceinline__ float kth_of_32(float v0, float v1, int k) {
 // overflows (ties at T), or a NaN, takes them off the row itself.
 // KT: at most as many best classes (0, 8 or 16: what fewer need takes fewer
 // registers).
+//
+// 4096 x 40001 bf16, best 8: 89 us for 328 MB (60 us at the card's copy rate; 79
+// without best classes; 4096 x 20000 fp32, the same bytes in half the values: 66
+// and 61): bound by vector operations, 10.5 issue slots a bf16 value for
+// unpacking, maximum and sums, four of them the exponential's.  (Keeping the chunk packed
+// and the rare ways out of the registers took 124 registers to 70 and 185 us to
+// 113; the threshold from 16 groups 108 to 97.)
 template <typename T, int L, int W, int E, int KT>
 __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
                                                          const int32_t* __restrict__ labels, int top_k, Outputs o,
@@ -393,6 +400,7 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
 // the lists' heads (as in k_scores_chunk) are out, the others are ranked.  Of
 // more parts, or where more than kRanked keys are left, they come off the heads
 // one by one: of 64 lists, or of 63 more and of the list so far (lane 63).
+// Latency: 7 us for 64 parts with 16 best classes (one by one: 10).
 template <typename T>
 __global__ __launch_bounds__(64) void k_scores_join(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
                                                     int parts, const int32_t* __restrict__ labels, int top_k,
@@ -496,6 +504,9 @@ __global__ __launch_bounds__(64) void k_scores_join(const T* __restrict__ z, int
 // insertion: bf16 as keys that hold the class too, one operation a place (a
 // value, class pair takes four); fp32 by strict comparisons from the lowest
 // class up, so that ties stay in order.  The first is left out of t.
+// 1,964,906 x 20 bf16, best 3: 39 us for 165 MB (30 at the copy rate); about 500
+// vector operations a row keep the SIMDs busy for some 30 of them.  (A wavefront
+// per row: 1380.)
 
 // A row of more than NP and at most NC classes as fp32, -inf past its end, in
 // pieces of 16 bytes.  A cut last piece runs into what follows the row (and is
@@ -684,7 +695,9 @@ __global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int
 // Which kernel takes rows of more than kRowMax classes, by their length (and,
 // for rows of several chunks, by how many rows there are): the fewest lanes
 // that hold the row at 32 values each, since what a team does once per row
-// (its reductions, the best classes' ranks) is as much work for 64 values as for 2048.
+// (its reductions, the best classes' ranks) is as much work for 64 values as for
+// 2048.  (40,000 rows of 512 and 513 bf16, best 8: 25 and 44 us; 20,000 of 2048
+// and 2049 fp32: 40 and 73.)
 struct Route {
   int lanes, per_lane;  // L W, E
   int parts;            // chunks of a row
@@ -693,20 +706,21 @@ Route route_of(int64_t n, int classes) {
   if (classes <= 512) return {16, 32, 1};
   if (classes <= 2048) return {64, 32, 1};
   if (classes <= 8192) return {256, 32, 1};
-  // chunks of 8192 once they are enough workgroups for 256 CUs, else four times as many
+  // chunks of 8192 once they are enough workgroups for 256 CUs, else four times
+  // as many (102 and 103 rows of 40001 bf16, best 8, one rule each: 14 and 13 us)
   const int big = (int)ceil_div(classes, 8192);
   return n * big >= 512 ? Route{256, 32, big} : Route{256, 8, (int)ceil_div(classes, 2048)};
 }
 
-// Whether one thread takes a row: of up to 64 classes; up to 128 in bf16, whose
-// best classes cost a thread less, and in fp32 where there are several
-// wavefronts of rows for every SIMD.  (16,383 x 70 bf16, best 8: 12 us by teams
-// of lanes; 65,536 x 128 fp32, best 8: 21 us by teams, 24 by threads; 600,000 x
-// 128: 194 and 117.)
+// Whether one thread takes a row: of up to 64 classes (300,000 x 64 fp32, best
+// 8: 36 us; x 65 by teams of lanes more than twice that); up to 128 in bf16,
+// whose best classes cost a thread less (16,383 x 70, best 8: 8 us, by teams
+// 12), and in fp32 where there is a wavefront of rows for every SIMD (65,536 x
+// 128, best 8: 24 us, by teams 21; 262,144 x 100, best 3: 33, by teams 66).
 constexpr int kRowMax = 64;
 template <typename T>
 bool by_thread(int64_t n, int classes) {
-  return classes <= kRowMax || (classes <= 128 && (sizeof(T) == 2 || n >= 1 << 18));
+  return classes <= kRowMax || (classes <= 128 && (sizeof(T) == 2 || n >= 1 << 16));
 }
 
 // f(NP, NC) for rows of more than NP and at most NC classes.
@@ -826,7 +840,8 @@ __device__ __forceinline__ float grad_direct(const GradRow& w, float x, float A)
 // wavefront go out through LDS, rows an odd number of words apart (each lane
 // its own bank), as consecutive words of 4 bytes (WORDS) or single values.
 // KT: at least top_k; the rows' best classes and their gradients come in
-// through LDS the same way.
+// through LDS the same way.  1,964,906 x 20 bf16: 43 us for 204 MB, 4.7 TB/s,
+// memory-bound (a wavefront per row: 520); with 4 best classes' gradients 72.
 template <typename T, int NP, int NC, bool WORDS, int KT>
 __global__ __launch_bounds__(64) void k_grad_rows(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
                                                   GradInputs q, T* __restrict__ dz, int64_t ldd, int stride,
@@ -901,7 +916,8 @@ __global__ __launch_bounds__(64) void k_grad_rows(const T* __restrict__ z, int64
 
 // Longer rows, teams as in k_scores_chunk, `span` values of a row to a team;
 // nothing is kept, so a team walks its span piece by piece.  Every 16 lanes
-// hold the row's best classes and their gradients, one a lane.
+// hold the row's best classes and their gradients, one a lane.  1024 x 40001
+// fp32: 65 us for 328 MB, 5.0 TB/s, memory-bound.
 template <typename T, int L, int W>
 __global__ __launch_bounds__(64 * W) void k_grad_chunk(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
                                                        int span, GradInputs q, T* __restrict__ dz, int64_t ldd) {
