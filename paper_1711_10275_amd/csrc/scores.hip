@@ -712,10 +712,9 @@ Route route_of(int64_t n, int classes) {
   return n * big >= 512 ? Route{256, 32, big} : Route{256, 8, (int)ceil_div(classes, 2048)};
 }
 
-// Whether one thread takes a row: of up to 64 classes (300,000 x 64 fp32, best
-// 8: 36 us; x 65 by teams of lanes more than twice that); up to 128 in bf16,
-// whose best classes cost a thread less (16,383 x 70, best 8: 8 us, by teams
-// 12), and in fp32 where there is a wavefront of rows for every SIMD (65,536 x
+// Whether one thread takes a row: of up to 64 classes; up to 128 in bf16, whose
+// best classes cost a thread less (16,383 x 70, best 8: 8 us, by teams of lanes
+// 12; 600,000 x 70: 73 and 222), and in fp32 where there is a wavefront of rows for every SIMD (65,536 x
 // 128, best 8: 24 us, by teams 21; 262,144 x 100, best 3: 33, by teams 66).
 constexpr int kRowMax = 64;
 template <typename T>

@@ -226,6 +226,30 @@ def test_graphs_and_streams(c):
                 assert torch.equal(a, b)
 
 
+def test_two_streams_at_once():
+    """Calls in flight together, each with its own inputs and workspace."""
+    units = []
+    for seed in (1, 2):
+        x, gamma, beta = draw(30000, 40, "f32", seed)
+        t = dev(x)
+        units.append((t, dev(gamma), dev(beta), stats_of(t, gamma, beta)[0]))
+
+    def calls(t, g, b, st):
+        a, q8 = sscn.batchnorm_relu_apply_q8(t, st, g, b)
+        return (a, q8.codes, *sscn.batchnorm_relu_backward_params_q8(t, q8, g, b, restore=True))
+    want = [calls(*u) for u in units]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for _ in range(5):
+        for st, u in zip(streams, units):
+            with torch.cuda.stream(st):
+                got.append(calls(*u))
+    torch.cuda.synchronize()
+    for i, out in enumerate(got):
+        for a, b in zip(out, want[i % 2]):
+            assert torch.equal(a, b)
+
+
 # ------------------------------------------------------------ a training step
 CH, NCLS = (8, 16, 24), 6
 

@@ -301,3 +301,25 @@ def test_graphs_and_streams(n, k):
         for g, out in graphs:
             for a, b in zip(out, want):
                 assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n,k", [(20000, 20), (40, 30000)])
+def test_two_streams_at_once(n, k):
+    """Calls in flight together, each with its own inputs and workspace."""
+    data = [(dev(z), dev(lab)) for z, lab in (draw(n, k, "f32", s) for s in (1, 2))]
+    one = torch.ones(n, device="cuda:0")
+
+    def calls(z, lab):
+        s = sscn.label_scores(z, lab, 3)
+        return (*s, sscn.label_scores_backward(z, s, lab, dlogprob=one))
+    want = [calls(*d) for d in data]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for _ in range(5):
+        for st, d in zip(streams, data):
+            with torch.cuda.stream(st):
+                got.append(calls(*d))
+    torch.cuda.synchronize()
+    for i, out in enumerate(got):
+        for a, b in zip(out, want[i % 2]):
+            assert torch.equal(a, b)
