@@ -694,10 +694,11 @@ __global__ __launch_bounds__(64) void k_scores_rows(const T* __restrict__ z, int
 
 // Which kernel takes rows of more than kRowMax classes, by their length (and,
 // for rows of several chunks, by how many rows there are): the fewest lanes
-// that hold the row at 32 values each, since what a team does once per row
-// (its reductions, the best classes' ranks) is as much work for 64 values as for
-// 2048.  (40,000 rows of 512 and 513 bf16, best 8: 25 and 44 us; 20,000 of 2048
-// and 2049 fp32: 40 and 73.)
+// that hold the row at 32 values each, or 64 within a wavefront, since what a
+// team does once per row (its reductions, the best classes' ranks) is as much
+// work for 64 values as for 2048.  (40,000 rows of 512 and 513 bf16, best 8: 25
+// and 44 us; 20,000 of 4096 and 4097: 61 and 72; 20,000 of 2049 fp32 by a
+// wavefront each 45, by four 73.)
 struct Route {
   int lanes, per_lane;  // L W, E
   int parts;            // chunks of a row
@@ -705,6 +706,7 @@ struct Route {
 Route route_of(int64_t n, int classes) {
   if (classes <= 512) return {16, 32, 1};
   if (classes <= 2048) return {64, 32, 1};
+  if (classes <= 4096) return {64, 64, 1};
   if (classes <= 8192) return {256, 32, 1};
   // chunks of 8192 once they are enough workgroups for 256 CUs, else four times
   // as many (102 and 103 rows of 40001 bf16, best 8, one rule each: 14 and 13 us)
@@ -769,6 +771,8 @@ sscn_status launch_scores(const T* z, int64_t ldz, int64_t n, int classes, const
     constexpr int KT = decltype(kt)::value;
     if (w.lanes == 16)
       k_scores_chunk<T, 16, 1, 32, KT><<<by_team, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
+    else if (w.lanes == 64 && w.per_lane == 64)
+      k_scores_chunk<T, 64, 1, 64, KT><<<by_team, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
     else if (w.lanes == 64)
       k_scores_chunk<T, 64, 1, 32, KT><<<by_team, 64, 0, s>>>(z, ldz, n, classes, labels, top_k, o, parts, keys);
     else if (w.per_lane == 32)

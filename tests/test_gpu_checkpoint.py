@@ -174,10 +174,12 @@ def test_no_rows():
     sscn.batchnorm_relu_backward_input_q8(dA, q8, one, one, one, dg, db, torch.empty_like(dA))
 
 
-def test_in_place_and_reused_buffers():
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("c,pad", [(48, 0), (70, 0), (70, 3), (33, 1)])
+def test_in_place_and_reused_buffers(c, pad, dtype):
     """y may be x, and dx may be the gradient added to it."""
-    x, gamma, beta = draw(500, 48, "f32", 8)
-    t = dev(x)
+    x, gamma, beta = draw(500, c, dtype, 8)
+    t = strided(x, dtype, pad)
     st, _ = stats_of(t, gamma, beta)
     a, q8 = sscn.batchnorm_relu_apply_q8(t, st, dev(gamma), dev(beta))
     a2, q2 = sscn.batchnorm_relu_apply_q8(t, st, dev(gamma), dev(beta), out=t)

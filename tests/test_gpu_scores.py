@@ -149,7 +149,7 @@ def check_grad(z, lab, top_k, dtype, zt, got, seed, parts="ght", pad=0):
 
 
 SIZES = [(1, 1, 1), (1, 2, 2), (5, 3, 0), (255, 20, 3), (257, 64, 16), (100, 65, 5), (33, 200, 8), (300, 129, 1),
-         (7, 1000, 16), (3, 5001, 4), (2, 40001, 8), (1, 131071, 16), (1, 131072, 0), (1030, 257, 2), (70, 8193, 3),
+         (7, 1000, 16), (5, 2049, 16), (9, 4096, 8), (3, 5001, 4), (2, 40001, 8), (1, 131071, 16), (1, 131072, 0), (1030, 257, 2), (70, 8193, 3),
          (300, 8200, 8), (2, 140001, 16), (1, 300001, 9), ((1 << 18) + 3, 66, 16)]
 
 
@@ -163,7 +163,7 @@ def test_scores_and_gradient(n, k, top_k, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("kind", ["masked", "lowest", "ties", "sure"])
-@pytest.mark.parametrize("n,k,top_k", [(300, 20, 16), (70, 50, 5), (40, 300, 16), (21, 1500, 16), (9, 9001, 16),
+@pytest.mark.parametrize("n,k,top_k", [(300, 20, 16), (70, 50, 5), (40, 300, 16), (21, 1500, 16), (12, 3001, 16), (9, 9001, 16),
                                        (260, 8193, 5), (3, 70003, 7), (1, 200000, 16)])
 def test_masks_ties_and_sure_rows(n, k, top_k, kind, dtype):
     z, lab = draw(n, k, dtype, n + k + len(kind), kind)
