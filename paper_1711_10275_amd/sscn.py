@@ -652,7 +652,11 @@ class LabelScores(NamedTuple):
 
 
 def _rows(t, name, dtype=None, device=None):
-    """_mat for rows that do not overlap, on one device."""
+    """_mat for rows that do not overlap, on one device.  Returns (address, ld)."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2:
+        (n, c), (ld, unit) = t.shape, t.stride()
+        if unit == 1 and ld >= c and (dtype is None or t.dtype is dtype) and (device is None or t.device == device):
+            return t.data_ptr(), ld
     p, ld = _mat(t, name, dtype)
     if device is not None and t.device != device:
         raise ValueError(f"{name} must be on {device}")
@@ -662,11 +666,16 @@ def _rows(t, name, dtype=None, device=None):
 
 
 def _on(t, name, dtype, shape, device):
-    """Pointer of a contiguous tensor of this type, shape and device."""
-    t = _dev_tensor(t, name, dtype)
-    if tuple(t.shape) != tuple(shape) or t.device != device:
-        raise ValueError(f"{name} must be a {tuple(shape)} tensor on {device}")
-    return ctypes.c_void_p(t.data_ptr())
+    """Address of a contiguous tensor of this type, shape and device."""
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.device == device
+            and t.is_contiguous() and t.is_cuda):
+        return t.data_ptr()
+    _dev_tensor(t, name, dtype)
+    raise ValueError(f"{name} must be a {tuple(shape)} tensor on {device}")
+
+
+def _at(t):
+    return t.data_ptr() if t is not None else None
 
 
 def _workspace(query, *sizes, device):
@@ -693,8 +702,8 @@ def label_scores(logits, labels=None, top_k=0):
     out = LabelScores(new(n) if labels is not None else None, new(n), new(n, 2),
                       new(n, top_k, dtype=torch.int32) if top_k else None, new(n, top_k) if top_k else None)
     with _device(dev):
-        _check(L.sscn_label_scores(zp, ldz, n, k, _dtype_code(logits), lp, top_k, *[_vp_of(t) for t in out],
-                                   _vp_of(work), work.numel() if work is not None else 0, _stream(logits)))
+        _check(L.sscn_label_scores(zp, ldz, n, k, _dtype_code(logits), lp, top_k, *map(_at, out),
+                                   _at(work), work.numel() if work is not None else 0, _stream(logits)))
     return out
 
 
@@ -739,7 +748,7 @@ def _q8(q8):
     if codes.dim() != 2:
         raise ValueError("codes must be n x c")
     n, c = codes.shape
-    return (ctypes.c_void_p(codes.data_ptr()),
+    return (codes.data_ptr(),
             _on(q8.exponents, "exponents", torch.uint8, (n, -(-c // Q8_BLOCK)), codes.device))
 
 
@@ -760,7 +769,7 @@ def batchnorm_relu_apply_q8(x, st, gamma, beta, out=None):
     with _device(dev):
         _check(lib().sscn_batchnorm_relu_apply_q8(xp, ldx, n, c, _dtype_code(x), v(st.mean, "mean"),
                                                   v(st.invstd, "invstd"), v(st.scale, "scale"), v(gamma, "gamma"),
-                                                  v(beta, "beta"), op, ldo, _vp_of(q8.codes), _vp_of(q8.exponents),
+                                                  v(beta, "beta"), op, ldo, _at(q8.codes), _at(q8.exponents),
                                                   _stream(x)))
     return out, q8
 
@@ -772,7 +781,7 @@ def q8_values(q8, dtype=torch.float32):
     n, c = q8.codes.shape
     out = torch.empty((n, c), dtype=dtype, device=q8.codes.device)
     with _device(out.device):
-        _check(lib().sscn_q8_values(*qp, n, c, _dtype_code(out), _vp_of(out), c, _stream(out)))
+        _check(lib().sscn_q8_values(*qp, n, c, _dtype_code(out), _at(out), c, _stream(out)))
     return out
 
 
@@ -792,8 +801,8 @@ def batchnorm_relu_backward_params_q8(dA, q8, gamma, beta, restore=False):
     work = _workspace(L.sscn_batchnorm_relu_backward_params_q8_workspace, n, c, device=dev)
     with _device(dev):
         _check(L.sscn_batchnorm_relu_backward_params_q8(dp, ldd, *qp, n, c, _dtype_code(dA), v(gamma, "gamma"),
-                                                        v(beta, "beta"), _vp_of(dg), _vp_of(db), _vp_of(a), c,
-                                                        _vp_of(work), work.numel(), _stream(dA)))
+                                                        v(beta, "beta"), _at(dg), _at(db), _at(a), c,
+                                                        _at(work), work.numel(), _stream(dA)))
     return dg, db, a
 
 
