@@ -531,9 +531,11 @@ sscn_status sscn_label_scores_backward(const void* logits, int64_t ldz, int64_t 
  * nearest whole number, ties to even, moved by one where the ReLU would
  * otherwise pass the restored value but not the original, or the other way
  * round: with gamma xhat' + beta > 0 for the mask, a backward pass from the
- * codes masks what the forward masked (where gamma * invstd does not
- * underflow).  A block in which some xhat is infinite or NaN has byte 255 and
- * stands for NaN in all its channels.
+ * codes masks what the forward masked (where gamma * invstd neither
+ * underflows nor overflows).  A block in which some xhat is infinite or NaN
+ * has byte 255 and stands for NaN in all its channels, whatever their codes.
+ * Every other byte and code is read as above, the caller's own too; a value
+ * beyond fp32 (of kept ones |xhat| from 63.5 * 2^122 up) reads as infinite.
  * None of these calls allocates: they can be captured into a graph.
  */
 

@@ -10,7 +10,7 @@
 // value.  Where rounding would carry a value over the ReLU's border, the code
 // is moved by one towards the side of the forward (127 is kept free for that):
 // the backward pass masks exactly what the forward masked.  A block that holds
-// an infinity or a NaN has the byte 255 and codes 0: 0 * inf, it stands for NaN.
+// an infinity or a NaN has the byte 255 and codes 0, and stands for NaN.
 #include <algorithm>
 #include <type_traits>
 
@@ -32,7 +32,13 @@ __device__ __forceinline__ uint32_t exponent_byte(uint32_t most) {
   if (most >= 0x7f800000u) return 255;
   return (uint32_t)max(1, (int)((most + 0x3ffffu) >> 23) - 6);
 }
-__device__ __forceinline__ float power(uint32_t byte) { return __uint_as_float(byte << 23); }  // 2^(byte - 127)
+__device__ __forceinline__ float power(uint32_t byte) { return __uint_as_float(byte << 23); }  // 2^(byte - 127), byte 1 .. 254
+// What a code of 1 stands for: 2^(byte - 127); the bit below the exponent makes
+// the byte 0 that (a subnormal number) too, and the byte 255 a NaN, so that
+// every code of its block is one.
+__device__ __forceinline__ float unit(uint32_t byte) {
+  return __uint_as_float(byte << 23 | (byte - 1 >= 254 ? 1u << 22 : 0));
+}
 
 // The ReLU's argument as the forward and as the backward pass forms it.
 __device__ __forceinline__ float pre_forward(float d, float scale, float beta) { return fmaf(d, scale, beta); }
@@ -123,8 +129,8 @@ __device__ __forceinline__ void store_piece(T* p, int valid, const float (&x)[kP
       if (i < valid) st(p + i, x[i]);
   }
 }
-// A piece's codes, and what they stand for: u 2^e - 128 2^e of the codes plus
-// 128 (exact, and NaN for the byte 255, whose power is inf).
+// A piece's codes, and what they stand for: code * 2^e, exact, and infinite only
+// where that is beyond fp32.
 template <int P, bool CUT>
 __device__ __forceinline__ void load_codes(const int8_t* p, int valid, uint32_t (&w)[P / 4]) {
   if (valid == P) {
@@ -141,9 +147,9 @@ __device__ __forceinline__ void load_codes(const int8_t* p, int valid, uint32_t 
 }
 template <int P>
 __device__ __forceinline__ void decode(const uint32_t (&w)[P / 4], uint32_t byte, float (&v)[P]) {
-  const float s = power(byte), off = -128.f * s;
+  const float s = unit(byte);
 #pragma unroll
-  for (int i = 0; i < P; ++i) v[i] = fmaf((float)((w[i / 4] ^ 0x80808080u) >> 8 * (i % 4) & 0xffu), s, off);
+  for (int i = 0; i < P; ++i) v[i] = (float)(int8_t)(w[i / 4] >> 8 * (i % 4)) * s;
 }
 // Per-channel constants of a piece.
 template <int P>
@@ -428,7 +434,7 @@ __global__ __launch_bounds__(256) void k_input_q8(const T* __restrict__ da, int6
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / cols;
     const int k = (int)(i - r * cols), col = col0 + k;
-    const float v = (float)codes[r * c + col] * power(exponents[r * blocks + col / kBlock]);
+    const float v = (float)codes[r * c + col] * unit(exponents[r * blocks + col / kBlock]);
     const float dz = pre_restored(v, gamma[col], beta[col]) > 0.f ? ld(da + r * ldd + col) : 0.f;
     float out = gamma[col] * invstd[col] * (dz - dbeta[col] * inv_n - v * (dgamma[col] * inv_n));
     if (add) out += ld(add + r * lda + k);
