@@ -505,9 +505,9 @@ sscn_status sscn_label_scores_workspace(int64_t n, int32_t classes, int32_t top_
  * (each of the three nullable) from what sscn_label_scores gave on the same
  * logits: stats, and entropy (with dentropy) and top_index (with dtop;
  * n x top_k, entries in [0, classes), a class listed twice receives both
- * gradients).  Rows without a label take nothing from dlogprob; a row of
- * -inf only gets zeros; a label >= classes (where dlogprob is given) makes
- * its row NaN.
+ * gradients).  Rows without a label take nothing from dlogprob; a label >=
+ * classes (where dlogprob is given) makes its row NaN; any other row of -inf
+ * only gets zeros.
  *   dlogits  n x classes in dtype, row stride ldd >= classes; overwritten,
  *            may not overlap the inputs; elements between the rows are left
  */

@@ -569,7 +569,8 @@ def label_scores(logits, labels, top_k=0):
 
 def label_scores_backward(logits, labels, dlogprob=None, dentropy=None, top=None, dtop=None):
     """Gradient of label_scores' numbers (weighted by dlogprob, dentropy and
-    dtop, the last for the classes `top`) at the logits."""
+    dtop, the last for the classes `top`) at the logits: NaN for a row whose
+    label is >= classes (with dlogprob), else 0 for a row of -inf only."""
     z = np.asarray(logits, np.float64)
     n, k = z.shape
     _, H, stats, _, _ = label_scores(z, None)
@@ -579,6 +580,7 @@ def label_scores_backward(logits, labels, dlogprob=None, dentropy=None, top=None
     A = np.zeros((n, k))
     if dlogprob is not None:
         labels = np.asarray(labels, np.int64)
+        empty &= labels < k
         g = np.where(labels < 0, 0.0, np.where(labels >= k, np.nan, dlogprob))
         A[np.arange(n), np.clip(labels, 0, k - 1)] += g
     if dtop is not None:

@@ -819,11 +819,12 @@ __device__ __forceinline__ GradRow grad_row(const GradInputs& q, int64_t r, int 
   GradRow w;
   const float2 st = reinterpret_cast<const float2*>(q.stats)[r];
   w.L = st.y;
-  w.empty = st.x == -INFINITY && st.y == 0.f;
-  w.base = w.empty ? 0.f : st.x;
+  w.lab = q.dlogprob ? q.labels[r] : -1;
+  const bool none = st.x == -INFINITY && st.y == 0.f;
+  w.empty = none && w.lab < classes;  // a label that is none makes the row NaN, as it does the log probability
+  w.base = none ? 0.f : st.x;
   w.h = q.dentropy ? q.dentropy[r] : 0.f;
   w.H = q.dentropy ? q.entropy[r] : 0.f;
-  w.lab = q.dlogprob ? q.labels[r] : -1;
   w.g = w.lab < 0 ? 0.f : w.lab >= classes ? NAN : q.dlogprob[r];
   w.G = w.g + direct;
   if (w.L != w.L) w.G = NAN;  // the clamp below would lose it

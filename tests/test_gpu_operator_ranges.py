@@ -97,3 +97,24 @@ def test_kept_values_near_the_types_end(dtype):
         np.testing.assert_array_equal(host(sscn.q8_values(q8)), O.q8_values(codes, exps).astype(np.float32))
     _, _, back = sscn.batchnorm_relu_backward_params_q8(torch.zeros_like(t), q8, dev(gamma), dev(beta), restore=True)
     assert torch.equal(a > 0, back > 0) and 0.2 < (a > 0).float().mean() < 0.8
+
+
+@pytest.mark.parametrize("k", [12, 100, 700, 3001])
+def test_a_label_that_is_none_in_a_row_that_allows_nothing(k):
+    """The label wins: the log probability and the gradient are NaN both."""
+    z = np.random.default_rng(k).standard_normal((8, k)).astype(np.float32)
+    z[::2] = -np.inf
+    lab = np.array([k, k, 0, 0, -1, -1, k + 5, 1], np.int32)
+    zt = dev(z)
+    got = sscn.label_scores(zt, dev(lab), 2)
+    g, t = np.ones(8, np.float32), np.ones((8, 2), np.float32)
+    for dtop in (None, t):
+        d = host(sscn.label_scores_backward(zt, got, dev(lab), dlogprob=dev(g), dtop=dev(dtop) if dtop is not None else None))
+        want = O.label_scores_backward(z, lab, g, None, host(got.top_index), dtop)
+        bad = lab >= k
+        np.testing.assert_array_equal(np.isnan(host(got.logprob)), bad)
+        assert np.isnan(d[bad]).all() and np.isnan(want[bad]).all()
+        assert (d[[2, 4]] == 0).all() and (want[[2, 4]] == 0).all()
+        assert np.abs(d[~bad] - want[~bad]).max() < 1e-5
+    # without a gradient at the log probabilities the label is not looked at
+    assert (host(sscn.label_scores_backward(zt, got, dev(lab), dentropy=dev(g)))[::2] == 0).all()
