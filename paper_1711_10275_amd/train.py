@@ -71,19 +71,23 @@ def _bn_relu(name, x, P, tape_entry, keep):
     return a
 
 
-def _unit_back(name, dy, e, rb, P, outs):
+def _unit_back(name, dy, e, rb, P, outs, traced):
     """Backward pass of one unit (or of the head).  outs: [(tensor, (lo, hi) or
     None, add or None)], column ranges of the gradient at the unit's input.
-    Returns (da, [dgamma, dbeta, dW]); from a kept q8, e["a"] becomes the
-    restored activations."""
+    Returns (da, [dgamma, dbeta, dW]).  The activations restored from a kept
+    q8 go once the weights' gradient has read them; `traced`, e["a"] holds
+    them."""
     gamma, beta = P.master[name][0], P.master[name][1]
     W, st = P.compute[name], e["st"]
     if "q8" in e:
         # the restored activations come out of the pass that the parameter
         # gradients make over dA and the codes, so dA first, then dW
         da, _ = sscn.sparse_conv_backward(None, W, dy, rb, wgrad=False)
-        dg, db, e["a"] = sscn.batchnorm_relu_backward_params_q8(da, e["q8"], gamma, beta, restore=True)
-        _, dW = sscn.sparse_conv_backward(e["a"], W, dy, rb, dgrad=False)
+        dg, db, a = sscn.batchnorm_relu_backward_params_q8(da, e["q8"], gamma, beta, restore=True)
+        _, dW = sscn.sparse_conv_backward(a, W, dy, rb, dgrad=False)
+        if traced:
+            e["a"] = a
+        del a
         for out, cols, add in outs:
             sscn.batchnorm_relu_backward_input_q8(da, e["q8"], gamma, beta, st.invstd, dg, db, out, add=add, cols=cols)
     else:
@@ -153,15 +157,18 @@ def train_step(x, labels, geom, P, lr=0.1, momentum=0.9, weight_decay=1e-4, upda
         scores = sscn.label_scores(logits, labels, top_k)
         loss, wanted = objective(scores)
         dlogits = sscn.label_scores_backward(logits, scores, labels, **wanted)
+        del scores, wanted
     dx = torch.empty_like(h)
     del h, z, skips  # what the tape does not keep goes now
 
     grads = {}
     dbias = sscn.column_sum(dlogits)
-    dz, grads["head"] = _unit_back("head", dlogits, head, geom.head, P, [(dx, None, None)])
+    traced = trace is not None
+    dz, grads["head"] = _unit_back("head", dlogits, head, geom.head, P, [(dx, None, None)], traced)
     grads["head"].append(dbias)
-    if trace is not None:
+    if traced:
         trace["head"] = dict(head, dy=dlogits, da=dz, dx=dx, logits=logits)
+    del dz, dlogits, logits, head  # nothing of the head is held through the units below
 
     def unit_back(dy, split=None, add=None):
         e = tape.pop()
@@ -174,8 +181,8 @@ def train_step(x, labels, geom, P, lr=0.1, momentum=0.9, weight_decay=1e-4, upda
         else:
             res = [new(hi - lo) for lo, hi in split]
             outs = [(r, cols, None) for r, cols in zip(res, split)]
-        da, grads[u.name] = _unit_back(u.name, dy, e, rb, P, outs)
-        if trace is not None:
+        da, grads[u.name] = _unit_back(u.name, dy, e, rb, P, outs, traced)
+        if traced:
             trace[u.name] = dict(e, dy=dy, da=da, dx=res)
         return res
 
@@ -183,8 +190,8 @@ def train_step(x, labels, geom, P, lr=0.1, momentum=0.9, weight_decay=1e-4, upda
     for l in range(L - 1):
         c = channels[l]
         dx = unit_back(dx)                                     # dec{l}b
-        dskip[l], dup = unit_back(dx, split=[(0, c), (c, 2 * c)])  # dec{l}a: [skip | up] halves
-        dx = unit_back(dup)                                    # up{l}: gradient at level l + 1
+        dskip[l], dx = unit_back(dx, split=[(0, c), (c, 2 * c)])  # dec{l}a: [skip | up] halves
+        dx = unit_back(dx)                                     # up{l}: gradient at level l + 1
     for l in reversed(range(L)):
         if l < L - 1:
             dx = unit_back(dx, add=dskip.pop(l))               # down{l}, plus the skip's gradient

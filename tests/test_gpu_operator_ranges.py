@@ -1,13 +1,15 @@
 """Ends of the ranges that the operators on a training step's two ends allow.
 Against the fp64 oracle."""
 import types
+import weakref
 
 import numpy as np
 import pytest
 import torch
 
 from oracle import sscn_oracle as O
-from paper_1711_10275_amd import sscn
+from paper_1711_10275_amd import sscn, train, unet
+from paper_1711_10275_amd import synthetic as S
 from tests.gpu_common import dev, host
 from tests.test_gpu_checkpoint import TD, U, half_step, strided
 
@@ -118,3 +120,36 @@ def test_a_label_that_is_none_in_a_row_that_allows_nothing(k):
         assert np.abs(d[~bad] - want[~bad]).max() < 1e-5
     # without a gradient at the log probabilities the label is not looked at
     assert (host(sscn.label_scores_backward(zt, got, dev(lab), dentropy=dev(g)))[::2] == 0).all()
+
+
+def test_a_training_step_lets_go_of_what_it_restored(monkeypatch):
+    """On kept codes a unit's restored activations go before its input's
+    gradient is written, and its dA before the next unit's: nothing of one
+    unit's backward pass is held through the next one's."""
+    restored, grads = [], []
+    params, inputs = sscn.batchnorm_relu_backward_params_q8, sscn.batchnorm_relu_backward_input_q8
+
+    def params_(dA, *a, **k):
+        assert not [1 for r in grads if r() is not None]
+        out = params(dA, *a, **k)
+        grads.append(weakref.ref(dA))
+        restored.append(weakref.ref(out[2]))
+        return out
+
+    def inputs_(*a, **k):
+        assert not [1 for r in restored if r() is not None]
+        return inputs(*a, **k)
+    monkeypatch.setattr(sscn, "batchnorm_relu_backward_params_q8", params_)
+    monkeypatch.setattr(sscn, "batchnorm_relu_backward_input_q8", inputs_)
+    n_classes, ch = 5, (8, 16)
+    coords = S.scenes_small(batch=1, L=32, target_per_sample=1000)
+    geom = train.Geometry(dev(coords), (32, 32, 32), levels=2)
+    P = train.Params(ch, n_classes, S.train_params)
+    x, lab = dev(S.features(coords.shape[0], ch[0], 1)), dev(S.labels(coords.shape[0], n_classes, 2))
+    train.train_step(x, lab, geom, P, update=False, keep="q8")
+    assert len(restored) == len(unet.units(ch)) + 1
+    # traced, the activations stay for the caller
+    monkeypatch.undo()
+    trace = {}
+    train.train_step(x, lab, geom, P, update=False, keep="q8", trace=trace)
+    assert all(e["a"].shape == e["da"].shape for e in trace.values())
