@@ -153,3 +153,30 @@ def test_a_training_step_lets_go_of_what_it_restored(monkeypatch):
     trace = {}
     train.train_step(x, lab, geom, P, update=False, keep="q8", trace=trace)
     assert all(e["a"].shape == e["da"].shape for e in trace.values())
+
+
+def test_a_row_of_as_many_classes_as_an_int_counts():
+    """The last chunk of a row of 2^31 - 1 logits: best classes from its list,
+    from the row itself (more equal logits than a list holds, a NaN), and the
+    gradient."""
+    k = 2 ** 31 - 1
+    z = torch.full((1, k), -float("inf"), dtype=torch.bfloat16, device="cuda:0")
+    at = [k - 1, 2 ** 30, 5]
+    for j, v in zip(at, (3.0, 2.0, 1.0)):
+        z[0, j] = v
+    lab = torch.tensor([k - 1], dtype=torch.int32, device="cuda:0")
+    got = sscn.label_scores(z, lab, 3)
+    want = O.label_scores(np.array([[3.0, 2.0, 1.0]]), [0], 3)
+    assert host(got.top_index).tolist() == [at]
+    for a, b in zip((got.logprob, got.entropy, got.stats, got.top_logprob), (want[0], want[1], want[2], want[4])):
+        assert np.abs(host(a) - b).max() < 1e-6
+    d = sscn.label_scores_backward(z, got, lab, dlogprob=torch.ones(1, device="cuda:0"))
+    grad = O.label_scores_backward(np.array([[3.0, 2.0, 1.0]]), [0], [1.0])
+    assert np.abs(host(d[0, torch.tensor(at, device="cuda:0")]) - grad).max() < 2 ** -8
+    assert int(torch.count_nonzero(d)) == 3
+    del d
+    z[0, k - 3000:] = 3.0
+    assert host(sscn.label_scores(z, lab, 2).top_index).tolist() == [[k - 3000, k - 2999]]
+    z[0, k - 2] = float("nan")
+    got = sscn.label_scores(z, lab, 2)
+    assert host(got.top_index).tolist() == [[k - 2, k - 3000]] and torch.isnan(got.entropy).all()
