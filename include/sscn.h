@@ -541,8 +541,9 @@ sscn_status sscn_label_scores_backward(const void* logits, int64_t ldz, int64_t 
 
 /*
  * sscn_batchnorm_relu_apply_q8 -- sscn_batchnorm_relu_apply (the same y, bit
- * for bit; y may be x, with its row stride) that also writes codes and exponents.  mean, invstd
- * and scale are those of sscn_batchnorm_forward.
+ * for bit; y may be x, with its row stride, or share no memory with it) that
+ * also writes codes and exponents.  mean, invstd and scale are those of
+ * sscn_batchnorm_forward.
  */
 sscn_status sscn_batchnorm_relu_apply_q8(const void* x, int64_t ldx, int64_t n, int32_t c, sscn_dtype dtype,
                                          const float* mean, const float* invstd, const float* scale,
@@ -577,7 +578,7 @@ sscn_status sscn_batchnorm_relu_backward_params_q8_workspace(int64_t n, int32_t 
  * for the channels [col0, col0 + cols) of the layer.  dA, the codes, the
  * exponents and the vectors are the whole layer's (c channels); add
  * (nullable) and dx hold the range's columns alone.  dx may be add (the same
- * row stride), not dA.
+ * row stride), else it shares no memory with add, nor with any of dA.
  */
 sscn_status sscn_batchnorm_relu_backward_input_q8(const void* dA, int64_t ldd, const int8_t* codes,
                                                   const uint8_t* exponents, int64_t n, int32_t c, int32_t col0,

@@ -507,6 +507,8 @@ extern "C" sscn_status sscn_batchnorm_relu_apply_q8(const void* x, int64_t ldx, 
     return fail(SSCN_ERR_INVALID_ARG, "q8: NULL mean, invstd, scale, gamma or beta");
   if (n == 0) return SSCN_OK;
   if (x == y && ldx != ldy) return fail(SSCN_ERR_INVALID_ARG, "q8: y in x's place with another row stride");
+  if (x != y && rows_share(x, ldx, c, y, ldy, c, n, dtype == SSCN_F32 ? 4 : 2))
+    return fail(SSCN_ERR_INVALID_ARG, "q8: y shares memory with x, but is not x");
   const int blocks = (int)ceil_div(c, kBlock);
   const dim3 g = place_grid(n, blocks, kRowGroups, dtype);
   return by_type(dtype, c, c, x == y, [&](auto t, auto cut, bool slide) {
@@ -549,7 +551,8 @@ extern "C" sscn_status sscn_batchnorm_relu_backward_params_q8(const void* da, in
   if (a) SSCN_TRY(check_rows(a, lda, n, c, dtype));
   SSCN_TRY(check_codes(codes, exponents, n));
   if (!gamma || !beta || !dgamma || !dbeta) return fail(SSCN_ERR_INVALID_ARG, "q8: NULL parameters or outputs");
-  if (n > 0 && a == da) return fail(SSCN_ERR_INVALID_ARG, "q8: a cannot replace dA");
+  if (n > 0 && (a == da || (a && rows_share(da, ldd, c, a, lda, c, n, dtype == SSCN_F32 ? 4 : 2))))
+    return fail(SSCN_ERR_INVALID_ARG, "q8: a cannot replace dA");
   int64_t need = 0;
   SSCN_TRY(sscn_batchnorm_relu_backward_params_q8_workspace(n, c, &need));
   if (workspace_bytes < need || !workspace || reinterpret_cast<uintptr_t>(workspace) % sizeof(double) != 0)
@@ -585,8 +588,12 @@ extern "C" sscn_status sscn_batchnorm_relu_backward_input_q8(const void* da, int
   if (!gamma || !beta || !invstd || !dgamma || !dbeta)
     return fail(SSCN_ERR_INVALID_ARG, "q8: NULL parameters or statistics");
   if (n == 0) return SSCN_OK;
-  if (dx == da) return fail(SSCN_ERR_INVALID_ARG, "q8: dx cannot replace dA");
+  const int64_t size = dtype == SSCN_F32 ? 4 : 2;
+  if (dx == da || rows_share(da, ldd, c, dx, ldx_out, cols, n, size))
+    return fail(SSCN_ERR_INVALID_ARG, "q8: dx cannot replace dA or columns of it");
   if (dx == add && ld_add != ldx_out) return fail(SSCN_ERR_INVALID_ARG, "q8: dx in add's place with another row stride");
+  if (add && dx != add && rows_share(add, ld_add, cols, dx, ldx_out, cols, n, size))
+    return fail(SSCN_ERR_INVALID_ARG, "q8: dx shares memory with add, but is not add");
   const int blocks = (int)ceil_div(c, kBlock);
   if (col0 % piece_of(dtype) == 0) {
     const dim3 g = place_grid(n, (int)ceil_div(cols, kBlock), kRowGroups, dtype);

@@ -228,6 +228,22 @@ sscn_status fill_f32(float* p, float v, int64_t count, hipStream_t s);
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Whether two matrices of n rows, of ca and cb elements of `size` bytes, share
+// memory.  Of one row stride the answer is exact (column ranges of one buffer
+// share none); rows of two strides are not looked into.
+inline bool rows_share(const void* a, int64_t lda, int64_t ca, const void* b, int64_t ldb, int64_t cb, int64_t n,
+                       int64_t size) {
+  if (n == 0 || (n > 1 && lda != ldb)) return false;
+  const int64_t d = ((intptr_t)b - (intptr_t)a), step = lda * size, wa = ca * size, wb = cb * size;
+  if (n == 1) return d < wa && -d < wb;
+  // row i of a meets row j of b where k = i - j has -wb < d - k step < wa
+  const int64_t past = d - wa;
+  int64_t k = past >= 0 ? past / step + 1 : -((-past - 1) / step);
+  for (; k * step < d + wb; ++k)
+    if (-n < k && k < n) return true;
+  return false;
+}
+
 // Workgroup i of a launch is dispatched to XCD i % kTileGroups.  Renumber a
 // grid of n workgroups so that each XCD takes one contiguous range of logical
 // items (bijective on [0, n)).

@@ -1097,7 +1097,8 @@ extern "C" sscn_status sscn_label_scores_backward(const void* logits, int64_t ld
   if (dlogprob && !labels) return fail(SSCN_ERR_INVALID_ARG, "scores: dlogprob without labels");
   if (dentropy && !entropy) return fail(SSCN_ERR_INVALID_ARG, "scores: dentropy without entropy");
   if (dtop && (top_k == 0 || !top_index)) return fail(SSCN_ERR_INVALID_ARG, "scores: dtop without top_index");
-  if (dlogits == logits) return fail(SSCN_ERR_INVALID_ARG, "scores: the gradient cannot replace the logits");
+  if (rows_share(logits, ldz, classes, dlogits, ldd, classes, n, dtype == SSCN_F32 ? 4 : 2) || dlogits == logits)
+    return fail(SSCN_ERR_INVALID_ARG, "scores: the gradient cannot replace the logits");
   const GradInputs q{labels, stats, entropy, dtop ? top_k : 0, top_index, dlogprob, dentropy, dtop};
   return dtype == SSCN_F32 ? launch_grad((const float*)logits, ldz, n, classes, q, (float*)dlogits, ldd, stream)
                            : launch_grad((const uint16_t*)logits, ldz, n, classes, q, (uint16_t*)dlogits, ldd, stream);

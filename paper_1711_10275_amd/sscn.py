@@ -709,7 +709,8 @@ def label_scores(logits, labels=None, top_k=0):
 
 def label_scores_backward(logits, scores, labels=None, dlogprob=None, dentropy=None, dtop=None, out=None):
     """dlogits of label_scores' numbers, given the gradients at its logprob
-    (n,), entropy (n,) and top_logprob (n, top_k), each fp32 or None."""
+    (n,), entropy (n,) and top_logprob (n, top_k), each fp32 or None.  out
+    shares no memory with the logits."""
     zp, ldz = _rows(logits, "logits")
     n, k = logits.shape
     dev, f32 = logits.device, torch.float32
@@ -754,7 +755,7 @@ def _q8(q8):
 
 def batchnorm_relu_apply_q8(x, st, gamma, beta, out=None):
     """batchnorm_relu_apply(x, st, beta) that also keeps the normalised input
-    in 8 bits -> (activations, Q8)."""
+    in 8 bits -> (activations, Q8).  out may be x."""
     xp, ldx = _rows(x, "x")
     n, c = x.shape
     dev = x.device
@@ -808,7 +809,8 @@ def batchnorm_relu_backward_params_q8(dA, q8, gamma, beta, restore=False):
 
 def batchnorm_relu_backward_input_q8(dA, q8, gamma, beta, invstd, dgamma, dbeta, out, add=None, cols=None):
     """out = gradient at the unit's input (columns `cols` = (lo, hi) of the
-    layer, default all) plus `add`; out / add hold just those columns."""
+    layer, default all) plus `add`; out / add hold just those columns.  out
+    may be add, and shares no memory with dA."""
     qp = _q8(q8)
     n, c = q8.codes.shape
     dev = q8.codes.device
