@@ -347,9 +347,9 @@ __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z
             }
           } else {
 #pragma nounroll
-            for (int k = all; k < x.len; k += L * W) {  // (k0 + k past the row could pass 2^31)
-              const float v = ld(row + k0 + k);
-              const uint64_t key = rank_key(v, (uint32_t)(k0 + k));
+            for (uint32_t k = k0 + all; k < (uint32_t)(k0 + x.len); k += L * W) {  // (past the row it may pass 2^31)
+              const float v = ld(row + k);
+              const uint64_t key = rank_key(v, k);
               if (!(v == -INFINITY) && key < last && key > best) best = key;
             }
           }
