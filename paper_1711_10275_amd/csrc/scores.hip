@@ -819,16 +819,18 @@ __device__ __forceinline__ GradRow grad_row(const GradInputs& q, int64_t r, int 
   GradRow w;
   const float2 st = reinterpret_cast<const float2*>(q.stats)[r];
   w.L = st.y;
-  w.lab = q.dlogprob ? q.labels[r] : -1;
-  const bool none = st.x == -INFINITY && st.y == 0.f;
-  w.empty = none && w.lab < classes;  // a label that is none makes the row NaN, as it does the log probability
-  w.base = none ? 0.f : st.x;
+  w.empty = st.x == -INFINITY && st.y == 0.f;
+  w.base = w.empty ? 0.f : st.x;
   w.h = q.dentropy ? q.dentropy[r] : 0.f;
   w.H = q.dentropy ? q.entropy[r] : 0.f;
+  w.lab = q.dlogprob ? q.labels[r] : -1;
   w.g = w.lab < 0 ? 0.f : w.lab >= classes ? NAN : q.dlogprob[r];
   w.G = w.g + direct;
   if (w.L != w.L) w.G = NAN;  // the clamp below would lose it
-  if (w.empty) w.g = w.G = w.h = 0.f;
+  if (w.empty) {
+    w.g = w.h = 0.f;
+    w.G = w.lab >= classes ? NAN : 0.f;  // the row's gradient, NaN where its log probability is
+  }
   return w;
 }
 __device__ __forceinline__ float grad_dense(const GradRow& w, float x) {
@@ -836,7 +838,7 @@ __device__ __forceinline__ float grad_dense(const GradRow& w, float x) {
   return -__builtin_amdgcn_exp2f(lp * 1.44269504088896340736f) * fmaf(w.h, lp + w.H, w.G);
 }
 __device__ __forceinline__ float grad_direct(const GradRow& w, float x, float A) {
-  if (w.empty) return 0.f;
+  if (w.empty) return w.G;
   const float lp = (x - w.base) - w.L, p = expf(lp);
   return -A * expm1f(lp) - p * ((w.G - A) + (p == 0.f ? 0.f : w.h * (lp + w.H)));
 }
