@@ -164,9 +164,10 @@ __device__ __forceinline__ void constants(const float* p, int valid, float (&k)[
 
 // Every kernel takes kRows of its rows a turn, so that their loads are in
 // flight together (1,964,906 x 32 fp32, one row: 158 us for the parameter
-// gradients with the activations, 115 with two).  All of them are bound by memory; at 1,964,906 x 32 bf16 (copy rate 5.5 TB/s): k_apply_q8 65 us
-// for 317 MB, 4.9 TB/s; k_q8_values 34 us for 191 MB, 5.5; k_params_q8 63 us for
-// 317 MB, 5.1; k_input_q8_pieces 60 us for 317 MB, 5.3.
+// gradients with the activations, 115 with two).  All of them are bound by
+// memory; at 1,964,906 x 32 bf16 (copy rate 5.5 TB/s): k_apply_q8 64 us for 317
+// MB, 4.9 TB/s; k_q8_values 33 us for 191 MB, 5.8; k_params_q8 62 us for 317 MB,
+// 5.1; k_input_q8_pieces 61 us for 317 MB, 5.2.
 constexpr int kRows = 2;
 
 template <typename T, bool CUT>
@@ -451,7 +452,8 @@ dim3 place_grid(int64_t n, int blocks, int64_t most, sscn_dtype dtype) {
   return dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div(n, rows), most)),
               (unsigned)ceil_div(blocks, span));
 }
-// Workgroups over the rows of the row-wise kernels: 256 CUs hold some 6 each.
+// Workgroups over the rows of the row-wise kernels: 8 to a CU, which holds 4 to 8
+// of them at once, by their registers.
 constexpr int64_t kRowGroups = 2048;
 
 // f(a value of the element type, whether pieces are cut, whether they slide) for

@@ -198,12 +198,15 @@ __device__ __forceinline__ float kth_of_32(float v0, float v1, int k) {
 // KT: at most as many best classes (0, 8 or 16: what fewer need takes fewer
 // registers).
 //
-// 4096 x 40001 bf16, best 8: 89 us for 328 MB (60 us at the card's copy rate; 79
-// without best classes; 4096 x 20000 fp32, the same bytes in half the values: 66
-// and 61): bound by vector operations, 10.5 issue slots a bf16 value for
-// unpacking, maximum and sums, four of them the exponential's.  (Keeping the chunk packed
-// and the rare ways out of the registers took 124 registers to 70 and 185 us to
-// 113; the threshold from 16 groups 108 to 97.)
+// 4096 x 40001 bf16 (328 MB, 60 us at the card's copy rate): 64 us without best
+// classes, memory-bound (10.5 issue slots a value for unpacking, maximum and sums
+// are 44 us of the vector units, behind other workgroups' loads), and the join's
+// 5; with the best 8, whose listing and ranking is work on top, 87 and 8.
+// (Keeping the chunk packed and the rare ways out of the registers took 124
+// registers to 70 and 185 us to 113; the threshold from 16 groups 108 to 97.)
+// Many equal logits at the threshold overflow the list, and the best classes come
+// off the row one by one: with all logits equal, best 8, 300,000 x 200 bf16 take
+// 422 us for 107, 4096 x 40001 1070 for 93.
 template <typename T, int L, int W, int E, int KT>
 __global__ __launch_bounds__(64 * W) void k_scores_chunk(const T* __restrict__ z, int64_t ldz, int64_t n, int classes,
                                                          const int32_t* __restrict__ labels, int top_k, Outputs o,
@@ -715,9 +718,16 @@ Route route_of(int64_t n, int classes) {
 }
 
 // Whether one thread takes a row: of up to 64 classes; up to 128 in bf16, whose
-// best classes cost a thread less (16,383 x 70, best 8: 8 us, by teams of lanes
-// 12; 600,000 x 70: 73 and 222), and in fp32 where there is a wavefront of rows for every SIMD (65,536 x
-// 128, best 8: 24 us, by teams 21; 262,144 x 100, best 3: 33, by teams 66).
+// best classes cost a thread less, and in fp32 where there is a wavefront of rows
+// for every SIMD.  By threads and by teams of 16 lanes, us (17 is the host's time
+// of a call, and what shorter kernels show):
+//   fp32                32,768 x 70  x 128    65,536 x 70  x 128    262,144 x 70   x 128
+//     best 3               17, 17    17, 17      17, 17    17, 18       23, 53     38, 62
+//     best 8               17, 17    19, 17      17, 20    21, 21       32, 62     51, 70
+//     best 16              17, 17    28, 19      21, 30    34, 31       50, 104    84, 113
+//   bf16, best 8           17, 18    17, 17      17, 30    17, 22       24, 97     31, 68
+//     best 16              17, 30    17, 20      17, 51    17, 36       28, 186    38, 126
+// (16,384 rows: 17 but for best 16: fp32 x 128 by threads 25, bf16 x 70 by teams 22.)
 constexpr int kRowMax = 64;
 template <typename T>
 bool by_thread(int64_t n, int classes) {
@@ -1012,6 +1022,17 @@ void launch_grad_rows(const T* z, int64_t ldz, int64_t n, int classes, const Gra
   else run(std::false_type{});
 }
 
+// Which kernel takes the gradient's rows, by their length: a thread, 16 lanes, a
+// wavefront, a workgroup per 2048 values.  Both sides of the lines, us, without
+// and with 4 best classes' gradients (fp32; bf16):
+//    64 classes, 300,000 rows: by threads 44, 57; 22, 32   by 16 lanes 55, 64; 40, 52
+//   512 classes,  40,000 rows: by 16 lanes 40, 46; 18, 21  by wavefronts 41, 45; 25, 30
+//   513 classes,  40,000 rows: by 16 lanes 55, 60; 25, 29  by wavefronts 47, 52; 31, 35
+//  2048 classes,  10,000 rows: by wavefronts 40, 43; 17, 19  (by workgroups from 1025 on: 36, 37; 22, 24)
+//  2049 classes,  10,000 rows: by wavefronts 48, 50; 23, 25  by workgroups 61, 65; 43, 47
+//  4096 classes,  10,000 rows: by wavefronts 78, 81; 38, 40  by workgroups 63, 67; 48, 53
+// The lines are fp32's, a little early above 2048; bf16's, of half the bytes, would
+// lie at some 1024 and past 4096.
 template <typename T>
 sscn_status launch_grad(const T* z, int64_t ldz, int64_t n, int classes, const GradInputs& q, T* dz, int64_t ldd,
                         hipStream_t s) {

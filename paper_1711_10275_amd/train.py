@@ -13,7 +13,7 @@ momentum 0.9, weight decay 1e-4, learning rate 0.1).
 Every arithmetic step runs in libsscn.so; this module orders the calls and
 keeps the tensors the backward pass needs: the batch statistics, and each
 unit's input and its pre-activated input (keep="full") or, in their place,
-its normalised input in 8 bits, from which the backward pass restores both
+its normalised input in 8 bits, which stands for both in the backward pass
 (keep="q8": a quarter of the bytes of a bf16 network's tape, an eighth of an
 fp32 one's).  Parameters are kept in
 fp32 (the master copy the update works on); a bf16 network convolves with a
