@@ -1,6 +1,7 @@
 """Ways through the kernels that need a shape of their own: a last piece that
 slides back in a range that starts inside the row, in bf16 rows at an odd
-stride, and outputs whose rows lie apart through the C entries."""
+stride, outputs whose rows lie apart through the C entries, and more rows than
+a launch has workgroups for."""
 import ctypes
 
 import numpy as np
@@ -59,3 +60,30 @@ def test_rows_apart_in_the_restored_outputs(n, c, ld, dtype):
                                                     stream) == 0
     assert torch.equal(wide[:, :c], a) and torch.equal(g2, dg) and torch.equal(b2, db)
     assert (wide[:, c:] == 7).all()
+
+
+# 4 rows to a workgroup, one row, a chunk of one row with and without a join,
+# each launched for fewer rows than these
+@pytest.mark.parametrize("n,k,dtype", [(131077, 129, "f32"), (131077, 129, "bf16"), (33001, 600, "f32"),
+                                       (16391, 4100, "bf16"), (16391, 8200, "bf16")])
+def test_more_rows_than_workgroups(n, k, dtype):
+    """Every row is what it is among fewer rows, bit for bit; among them rows
+    of equal logits, with a NaN and with none allowed."""
+    g = torch.Generator(device="cuda:0").manual_seed(k)
+    z = torch.randn(n, k, generator=g, device="cuda:0").to(TD[dtype])
+    z[5::97] = 1.5
+    z[6::89, k // 3] = float("nan")
+    z[7::83] = -float("inf")
+    z[8::79, ::2] = -float("inf")
+    lab = torch.randint(-1, k, (n,), generator=g, device="cuda:0", dtype=torch.int32)
+    w, t = torch.randn(n, generator=g, device="cuda:0"), torch.randn(n, 5, generator=g, device="cuda:0")
+
+    def calls(at):
+        s = sscn.label_scores(z[at], lab[at], 5)
+        return (*s, sscn.label_scores_backward(z[at], s, lab[at], dlogprob=w[at], dentropy=w[at], dtop=t[at]))
+    bits = lambda x: x.contiguous().view({1: torch.int8, 2: torch.int16, 4: torch.int32}[x.element_size()])
+    whole = calls(slice(0, n))
+    for lo in range(0, n, 4096):
+        at = slice(lo, min(n, lo + 4096)) if n - lo > 300 else slice(n - 300, n)
+        for a, b in zip(whole, calls(at)):
+            assert torch.equal(bits(a[at]), bits(b)), lo
