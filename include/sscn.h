@@ -481,11 +481,13 @@ sscn_status sscn_softmax_nll(const void* logits, int64_t n, int32_t classes, ssc
  *            have no effect)
  *   labels   device int32, n; NULL with logprob NULL: no labels
  *   top_k    0 .. min(16, classes); 0: top_index and top_logprob are not used
- * Numbers are computed and written in fp32.  A class of logit -inf is
- * excluded (log p = -inf); a row of nothing else has entropy 0, stats
- * (-inf, 0) and every log p = -inf.  A NaN or +inf makes its row's entropy,
- * L and log probabilities NaN.  Outputs are contiguous and may not overlap
- * the inputs.  The same call gives the same bits.
+ * Numbers are computed and written in fp32; a class whose exp(x - m) is below
+ * 2^-126 adds nothing to the sums (nor, its p below that, takes any gradient
+ * through p).  A class of logit -inf is excluded (log p = -inf); a row of
+ * nothing else has entropy 0, stats (-inf, 0) and every log p = -inf.  A NaN
+ * or +inf makes its row's entropy, L and log probabilities NaN.  Outputs are
+ * contiguous and may not overlap the inputs.  The same call gives the same
+ * bits.
  *   workspace  device, 16-byte aligned, at least the bytes that
  *              sscn_label_scores_workspace gives for these n, classes and
  *              top_k (0: may be NULL), the call's own until its work is done

@@ -117,7 +117,7 @@ __device__ __forceinline__ float2 finish(const Part& p) {
 // Sums of e^(x - m) and e^(x - m) (x - m) as powers of two, h = (x - m) log2(e).
 // h is one rounded product: a term is off by up to 2.25 |x - m| half steps,
 // which its own size e^(x - m) outweighs; forming the product's low part too
-// would cost three more operations a value.
+// would cost three more operations a value.  Below 2^-126 the power of two is 0.
 struct ExpSums {
   float base, s = 0.f, a = 0.f;
   __device__ explicit ExpSums(float m) : base(m == -INFINITY ? 0.f : m) {}
